@@ -1,0 +1,348 @@
+"""Cases and plain forms of the operators that regularise and place the Vision Transformer's block (include/cnnk_rel.h):
+dropout from a counter-based generator with the bias and the residual sum around it, and self-attention with a learned
+relative position bias, dropout of the probabilities, padded batches and masked pairs.
+
+`own` false: elementary torch operations in 32 bits.  `own` true: the library's entry points, as a user calls them."""
+import math
+
+import torch
+
+own = False
+
+DEV = "cuda"
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+M32 = 0xFFFFFFFF
+
+
+def listed():
+    drop = lambda name, **k: dict(dict(name=name, op="drop", dtype="bf16", p=0.1, span=0, bias=True, res=True, train=True), **k)
+    attn = lambda name, **k: dict(dict(name=name, op="attn", dtype="bf16", B=64, gh=14, gw=14, cls=1, heads=12, dh=64, p=0.1, train=True,
+                                       ragged=False, window=0), **k)
+    return [
+        # the small transformer of the tests (four images of 17 tokens, width 128): launch latency
+        drop("drop_mini_f32", dtype="f32", rows=4 * 17, C=128),
+        # behind the attention projection of ViT-B/16 at batch 64, both directions with the projection's bias gradient
+        drop("drop_b16_b64", rows=64 * 197, C=768),
+        # stochastic depth: one draw for each image, no bias
+        drop("path_b16_b64", rows=64 * 197, C=768, span=197, bias=False, p=0.2),
+        # images of 384 x 384 at batch 64 in fp32, width 1024: the largest tensor
+        drop("drop_384_f32", dtype="f32", rows=64 * 577, C=1024),
+        # one small image in evaluation: latency
+        attn("attn_one_eval", B=1, gh=7, gw=7, heads=3, p=0.0, train=False),
+        # the small transformer of the tests, fp32 storage
+        attn("attn_mini_f32", dtype="f32", B=4, gh=4, gw=4, heads=2),
+        # validation of ViT-B/16, batch 8
+        attn("attn_b16_b8_eval", B=8, p=0.0, train=False),
+        # ViT-B/16 training, batch 8 and batch 64
+        attn("attn_b16_b8", B=8),
+        attn("attn_b16_b64"),
+        # fine-tuning at 384 x 384
+        attn("attn_384_b16", B=16, gh=24, gw=24),
+        # images of several sizes padded to one length, attention within windows, heads of 32
+        attn("attn_ragged_dh32", B=24, gh=19, gw=21, cls=0, heads=16, dh=32, ragged=True, window=5),
+        # one large image, 64 x 64 patches
+        attn("attn_long", B=1, gh=64, gw=64, cls=0, p=0.0),
+    ]
+
+
+def draw(rng):
+    log = lambda a, b: int(round(math.exp(rng.uniform(math.log(a), math.log(b)))))
+    p = rng.choice([0.0, 0.1, 0.2, round(rng.uniform(0.01, 0.6), 3)])
+    if rng.random() < 0.4:
+        rows = log(1, 36000)
+        span = rng.choice([0, 0, 1, 50, 197, rows])
+        return dict(op="drop", dtype=rng.choice(["bf16", "bf16", "f32"]), rows=rows, C=8 * log(1, 128), p=p, span=span, bias=rng.random() < 0.6,
+                    res=rng.random() < 0.7, train=rng.random() < 0.7)
+    side = log(1, 40)
+    gh, gw = side, max(1, side + rng.randint(-2, 3))
+    heads, dh, f32 = rng.choice([1, 2, 3, 6, 12, 16]), rng.choice([16, 32, 64, 64, 128]), rng.random() < 0.25
+    most = (4e7 if f32 else 2e8) * min(1, 64 / dh) / (heads * (gh * gw + 1) ** 2)
+    return dict(op="attn", dtype="f32" if f32 else "bf16", B=log(1, max(1, min(64, int(most)))), gh=gh, gw=gw, cls=rng.randint(0, 1), heads=heads, dh=dh,
+                p=p, train=rng.random() < 0.7, ragged=rng.random() < 0.4, window=rng.choice([0, 0, 2, 7]))
+
+
+def tokens(case):
+    return case["gh"] * case["gw"] + case["cls"]
+
+
+def lengths(case):
+    """Tokens of each image: all of them, or spread from a quarter of them to all."""
+    T, B = tokens(case), case["B"]
+    return [T - (T - T // 4) * i // B for i in range(B)] if case["ragged"] else [T] * B
+
+
+def buckets_of(case):
+    return (2 * case["gh"] - 1) * (2 * case["gw"] - 1) + 3 * case["cls"]
+
+
+def bucket_map(case):
+    """Bucket of query t and key u, [T][T]: their offset in rows and columns, three more for pairs with the class token; -1
+    where an offset is over the window."""
+    gh, gw, c, w = case["gh"], case["gw"], case["cls"], case["window"]
+    i = torch.arange(gh * gw, device=DEV, dtype=torch.int32)
+    y, x = i // gw, i % gw
+    dy, dx = y[:, None] - y[None, :], x[:, None] - x[None, :]
+    m = (dy + (gh - 1)) * (2 * gw - 1) + dx + (gw - 1)
+    if w:
+        m[(dy.abs() > w) | (dx.abs() > w)] = -1
+    if not c:
+        return m.contiguous()
+    n = (2 * gh - 1) * (2 * gw - 1)
+    full = torch.full((gh * gw + 1, gh * gw + 1), n, device=DEV, dtype=torch.int32)
+    full[1:, 0] = n + 1
+    full[0, 0] = n + 2
+    full[1:, 1:] = m
+    return full
+
+
+def prepare(case, seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    t = TYPES[case["dtype"]]
+    rand = lambda *s: torch.randn(*s, device=DEV, generator=g)
+    s = dict(case)
+    rng = torch.randint(-(1 << 62), 1 << 62, (2,), device=DEV, generator=g, dtype=torch.int64)
+    rng[1] = seed % 100003
+    s["rng"], s["site"] = rng, 7
+    if case["op"] == "drop":
+        R, C = case["rows"], case["C"]
+        s["z"], s["dy"] = rand(R, C).to(t), rand(R, C).to(t)
+        s["b"] = rand(C) * 0.5 if case["bias"] else None
+        s["r"] = rand(R, C).to(t) if case["res"] else None
+    else:
+        B, T, H, dh = case["B"], tokens(case), case["heads"], case["dh"]
+        s["qkv"], s["d_o"] = rand(B, T, 3 * H * dh).to(t), (rand(B, T, H * dh) * 0.1).to(t)
+        s["table"] = rand(buckets_of(case), H) * 0.5
+        s["map"] = bucket_map(case)
+        s["lens"] = None
+        if case["ragged"]:
+            order = torch.randperm(B, generator=g, device=DEV)
+            s["lens"] = torch.tensor(lengths(case), dtype=torch.int32, device=DEV)[order].contiguous()
+    if own:      # what a user's program keeps: descriptor, plan of the map, output buffers, workspace
+        from paper_2503_23186_amd import cnnk, rel
+        d = cnnk.BF16 if case["dtype"] == "bf16" else cnnk.F32
+        stream = torch.cuda.current_stream().cuda_stream
+        buf = lambda n: torch.empty(max(256, int(n)), dtype=torch.uint8, device=DEV)
+        if case["op"] == "drop":
+            s["desc"] = rel.dropout_desc(R, C, d, case["p"], 7, case["span"])
+            s["y"], s["dz"] = torch.empty_like(s["z"]), torch.empty_like(s["z"])
+            s["dbias"] = torch.empty(C, device=DEV)
+            s["ws"] = buf(rel.cnnk_dropout_workspace_bytes(s["desc"]))
+        else:
+            n = buckets_of(case)
+            s["desc"] = rel.rel_desc(B, T, H, dh, d, n, case["p"], 7)
+            s["plan"] = buf(rel.cnnk_rel_plan_bytes(T, n))
+            ws = buf(rel.cnnk_rel_plan_workspace_bytes(T, n))
+            rel.cnnk_rel_plan(T, n, s["map"], s["plan"], ws, ws.numel(), stream)
+            s["o"], s["o_rest"] = torch.empty(B, T, H * dh, dtype=t, device=DEV), None
+            if case["train"]:
+                s["o_rest"] = torch.empty_like(s["o"]) if case["dtype"] == "bf16" else None
+                s["stats"] = torch.empty(B, H, T, 2, device=DEV)
+                s["dqkv"], s["dtable"] = torch.empty_like(s["qkv"]), torch.empty_like(s["table"])
+                s["ws"] = buf(rel.cnnk_rel_attention_workspace_bytes(s["desc"]))
+    return s
+
+
+def run(s):
+    if own:
+        return run_own(s)
+    return plain_drop(s) if s["op"] == "drop" else plain_attention(s)
+
+
+def run_own(s):
+    from paper_2503_23186_amd import rel
+    stream = torch.cuda.current_stream().cuda_stream
+    if s["op"] == "drop":
+        rel.cnnk_dropout_fwd(s["desc"], s["z"], s["b"], s["r"], s["rng"], s["y"], stream)
+        if not s["train"]:
+            return s["y"]
+        db = s["dbias"] if s["bias"] else None
+        rel.cnnk_dropout_bwd(s["desc"], s["dy"], s["rng"], s["dz"], db, s["ws"], s["ws"].numel(), stream)
+        return [s["y"], s["dz"]] + ([db] if s["bias"] else [])
+    if not s["train"]:
+        rel.cnnk_rel_attention_fwd(s["desc"], s["qkv"], s["table"], s["plan"], s["lens"], s["rng"], s["o"], None, None, stream)
+        return s["o"]
+    rel.cnnk_rel_attention_fwd(s["desc"], s["qkv"], s["table"], s["plan"], s["lens"], s["rng"], s["o"], s["o_rest"], s["stats"], stream)
+    rel.cnnk_rel_attention_bwd(s["desc"], s["qkv"], s["o"], s["o_rest"], s["d_o"], s["table"], s["plan"], s["lens"], s["rng"], s["stats"], s["dqkv"],
+                               s["dtable"], s["ws"], s["ws"].numel(), stream)
+    return [s["o"], s["dqkv"], s["dtable"]]
+
+
+# ---- plain forms -----------------------------------------------------------------------------------------
+
+def philox(c0, c1, c2, c3, k0, k1):
+    """Philox4x32 with seven rounds (J. Salmon, M. Moraes, R. Dror, D. Shaw, SC 2011) on 32-bit words held in int64."""
+    for i in range(7):
+        a, b = c0 * 0xD2511F53, c2 * 0xCD9E8D57
+        c0, c1, c2, c3 = ((b >> 32) & M32) ^ c1 ^ k0, b & M32, ((a >> 32) & M32) ^ c3 ^ k1, a & M32
+        k0, k1 = (k0 + 0x9E3779B9) & M32, (k1 + 0xBB67AE85) & M32
+    return c0, c1, c2, c3
+
+
+def site_key(rng, site):
+    """The key that a call site has in this step, from the state (seed, step)."""
+    zero = torch.zeros_like(rng[0])
+    k = philox(rng[1] & M32, (rng[1] >> 32) & M32, zero + site, zero, rng[0] & M32, (rng[0] >> 32) & M32)
+    return k[0], k[1]
+
+
+def threshold(p):
+    return int(math.floor(p * 65536 + 0.5))
+
+
+def kept_elements(n, tag, q, key):
+    """Whether elements 0..n-1 are kept: eight 16-bit draws of a call to eight elements."""
+    i = torch.arange((n + 7) // 8, device=DEV)
+    w = torch.stack(philox(i & M32, i >> 32, torch.zeros_like(i), torch.full_like(i, tag), *key), 1)
+    return (torch.stack((w & 0xFFFF, w >> 16), 2).reshape(-1)[:n] >= q)
+
+
+def kept_pairs(bh, T, q, key):
+    """Whether query t's probability of key u is kept, [bh][T][T]: a call's four words to four queries, their halves to two keys."""
+    u, t, z = torch.arange((T + 1) // 2, device=DEV), torch.arange((T + 3) // 4, device=DEV), torch.arange(bh, device=DEV)
+    c = torch.broadcast_tensors(u[None, None, :], t[None, :, None], z[:, None, None])
+    w = torch.stack(philox(*c, torch.full_like(c[0], 2), *key), 2)                   # [bh][T/4][4][T/2]
+    return torch.stack((w & 0xFFFF, w >> 16), 4).reshape(bh, 4 * len(t), 2 * len(u))[:, :T, :T] >= q
+
+
+def plain_drop(s):
+    R, C, q = s["rows"], s["C"], threshold(s["p"])
+    key, scale = site_key(s["rng"], s["site"]), 65536.0 / (65536 - q)
+    if s["span"]:
+        keep = kept_elements((R + s["span"] - 1) // s["span"], 1, q, key).repeat_interleave(s["span"])[:R, None]
+    else:
+        keep = kept_elements(R * C, 0, q, key).reshape(R, C)
+    t = s["z"].dtype
+    y = s["z"].float()
+    if s["bias"]:
+        y = y + s["b"]
+    y = torch.where(keep, y * scale, 0.0)
+    if s["res"]:
+        y = y + s["r"].float()
+    if not s["train"]:
+        return y.to(t)
+    dz = torch.where(keep, s["dy"].float() * scale, 0.0)
+    return [y.to(t), dz.to(t)] + ([dz.sum(0, dtype=torch.float64).float()] if s["bias"] else [])
+
+
+def plain_attention(s):
+    B, H, dh = s["B"], s["heads"], s["dh"]
+    T, t, q = s["qkv"].shape[1], s["qkv"].dtype, threshold(s["p"])
+    qkv = s["qkv"].float().reshape(B, T, 3, H, dh).permute(2, 0, 3, 1, 4).contiguous()
+    Q, K, V = qkv[0], qkv[1], qkv[2]
+    seen = s["map"] >= 0
+    bias = s["table"][s["map"].clamp(min=0).long()].permute(2, 0, 1)
+    x = torch.matmul(Q, K.transpose(2, 3).contiguous()) * (1.0 / math.sqrt(dh)) + bias
+    if s["lens"] is not None:
+        in_row = torch.arange(T, device=DEV)[None, :] < s["lens"][:, None]
+        seen = seen & (in_row[:, None, None, :] & in_row[:, None, :, None])
+    x = torch.where(seen, x, -math.inf)
+    m = x.amax(-1, keepdim=True)
+    e = torch.where(seen, torch.exp(x - m), 0.0)
+    total = e.sum(-1, keepdim=True)
+    P = torch.where(total > 0, e / total, 0.0)
+    if q:
+        keep = kept_pairs(B * H, T, q, site_key(s["rng"], s["site"])).reshape(B, H, T, T)
+        scale = 65536.0 / (65536 - q)
+        D = torch.where(keep, P * scale, 0.0)
+    else:
+        D = P
+    O = torch.matmul(D, V)
+    back = lambda a: a.permute(0, 2, 1, 3).reshape(B, T, H * dh).to(t)
+    if not s["train"]:
+        return back(O)
+    G = s["d_o"].float().reshape(B, T, H, dh).permute(0, 2, 1, 3).contiguous()
+    dV = torch.matmul(D.transpose(2, 3).contiguous(), G)
+    dP = torch.matmul(G, V.transpose(2, 3).contiguous())
+    if q:
+        dP = torch.where(keep, dP * scale, 0.0)
+    dx = P * (dP - (P * dP).sum(-1, keepdim=True))
+    dQ = torch.matmul(dx, K) * (1.0 / math.sqrt(dh))
+    dK = torch.matmul(dx.transpose(2, 3).contiguous(), Q) * (1.0 / math.sqrt(dh))
+    pairs = dx.sum(0, dtype=torch.float64).reshape(H, T * T)
+    ids = s["map"].reshape(-1).long()
+    dtable = torch.zeros(s["table"].shape[0] + 1, H, dtype=torch.float64, device=DEV)
+    dtable.index_add_(0, torch.where(ids >= 0, ids, s["table"].shape[0]), pairs.t().contiguous())
+    dqkv = torch.stack((dQ, dK, dV), 0).permute(1, 3, 0, 2, 4).reshape(B, T, 3 * H * dh).to(t)
+    return [back(O), dqkv, dtable[:-1].float()]
+
+
+# ---- work and exact results --------------------------------------------------------------------------------
+
+def work(case):
+    size = 2 if case["dtype"] == "bf16" else 4
+    if case["op"] == "drop":
+        n = case["rows"] * case["C"]
+        return {"bytes": n * size * (2 + case["res"] + 2 * case["train"]) + 8 * case["C"] * case["bias"], "flops": 3 * n * (1 + case["train"])}
+    n, row, T = sum(lengths(case)), case["heads"] * case["dh"], tokens(case)
+    pairs = sum(t * t for t in lengths(case)) * row
+    move = 4 * n * row * size + 4 * (T * T + buckets_of(case) * case["heads"])
+    if case["train"]:      # the backward pass reads q, k, v, the output and its gradient, and writes the gradients of q, k and v
+        move += 8 * n * row * size + 4 * (T * T + 2 * buckets_of(case) * case["heads"])
+    return {"bytes": move, "flops": (14 if case["train"] else 4) * pairs}
+
+
+def words64(c, key):
+    """The generator again, with products from 16-bit pieces."""
+    def product(a, b):
+        al, ah, bl, bh = a & 0xFFFF, a >> 16, b & 0xFFFF, b >> 16
+        mid = (al * bl >> 16) + (ah * bl & 0xFFFF) + (al * bh & 0xFFFF)
+        low = (al * bl & 0xFFFF) | ((mid & 0xFFFF) << 16)
+        return ah * bh + (ah * bl >> 16) + (al * bh >> 16) + (mid >> 16), low
+    x, (ka, kb) = list(c), key
+    for i in range(7):
+        h0, l0 = product(x[0], 0xD2511F53)
+        h1, l1 = product(x[2], 0xCD9E8D57)
+        x = [h1 ^ x[1] ^ ((ka + i * 0x9E3779B9) % (1 << 32)), l1, h0 ^ x[3] ^ ((kb + i * 0xBB67AE85) % (1 << 32)), l0]
+    return x
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    q = int(math.floor(case["p"] * 65536 + 0.5))
+    keep_scale = 1.0 / (1.0 - q / 65536.0)
+    seed64, step = (int(v) % (1 << 64) for v in s["rng"].tolist())
+    k = words64([torch.tensor(v) for v in (step % (1 << 32), step >> 32, s["site"], 0)], (seed64 % (1 << 32), seed64 >> 32))
+    key = (int(k[0]), int(k[1]))
+    if case["op"] == "drop":
+        R, C = case["rows"], case["C"]
+        at = torch.arange(R, device=DEV)[:, None] // case["span"] if case["span"] else torch.arange(R * C, device=DEV).reshape(R, C)
+        call, part = at // 8, at % 8
+        w = words64([call % (1 << 32), call >> 32, torch.zeros_like(call), torch.full_like(call, 1 if case["span"] else 0)], key)
+        word = torch.where(part < 4, torch.where(part < 2, w[0], w[1]), torch.where(part < 6, w[2], w[3]))
+        keep = ((word >> (16 * (part % 2))) % 65536 >= q).double() * keep_scale
+        y = keep * (s["z"].double() + (s["b"].double() if case["bias"] else 0.0))
+        y = y + s["r"].double() if case["res"] else y
+        dz = keep * s["dy"].double()
+        return [y, dz] + ([dz.sum(0)] if case["bias"] else []) if case["train"] else y
+    B, T, H, dh = case["B"], tokens(case), case["heads"], case["dh"]
+    qkv, g = s["qkv"].double().reshape(B, T, 3, H, dh), s["d_o"].double().reshape(B, T, H, dh)
+    n = torch.full((B,), T, device=DEV) if s["lens"] is None else s["lens"]
+    at = torch.arange(T, device=DEV)
+    o, dqkv, dtable = torch.zeros(B, T, H, dh, dtype=torch.float64, device=DEV), torch.zeros_like(qkv), torch.zeros_like(s["table"], dtype=torch.float64)
+    ids = s["map"].long()
+    for b in range(B):
+        ok = (ids >= 0) & (at[:, None] < n[b]) & (at[None, :] < n[b])
+        for h in range(H):
+            leaf = [qkv[b, :, i, h].clone().requires_grad_(case["train"]) for i in range(3)] + [s["table"][:, h].double().requires_grad_(case["train"])]
+            with torch.set_grad_enabled(case["train"]):
+                # the reference is the largest score of a row; it cancels, so it takes no part in the derivative
+                x = leaf[0] @ leaf[1].t() / dh ** 0.5 + leaf[3][ids.clamp(min=0)]
+                top = torch.where(ok, x, -1e300).max(1, keepdim=True).values.detach()
+                e = torch.where(ok, (torch.where(ok, x, top) - top).exp(), torch.zeros_like(x))
+                p = e / (e.sum(1, keepdim=True) + (~ok.any(1, keepdim=True)).double())
+                if q:
+                    u, t = torch.broadcast_tensors(at[None, :], at[:, None])
+                    w = words64([u // 2, t // 4, torch.full_like(u, b * H + h), torch.full_like(u, 2)], key)
+                    r = t % 4
+                    word = torch.where(r == 0, w[0], torch.where(r == 1, w[1], torch.where(r == 2, w[2], w[3])))
+                    p = p * ((word >> (16 * (u % 2))) % 65536 >= q).double() * keep_scale
+                out = p @ leaf[2]
+            o[b, :, h] = out.detach()
+            if case["train"]:
+                d = torch.autograd.grad(out, leaf, g[b, :, h])
+                for i in range(3):
+                    dqkv[b, :, i, h] = d[i]
+                dtable[:, h] += d[3]
+    o = o.reshape(B, T, H * dh)
+    return [o, dqkv.reshape(B, T, 3 * H * dh), dtable] if case["train"] else o
