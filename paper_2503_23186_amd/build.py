@@ -20,7 +20,8 @@ def sources():
 
 def _newest_header():
     hs = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".h")]
-    hs.append(os.path.join(HERE, "..", "include", "cnnk.h"))
+    inc = os.path.join(HERE, "..", "include")
+    hs += [os.path.join(inc, f) for f in os.listdir(inc)]
     return max(os.path.getmtime(h) for h in hs)
 
 

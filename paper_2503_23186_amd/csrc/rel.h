@@ -1,0 +1,65 @@
+// What the kernels behind include/cnnk_rel.h share: the generator of dropout, the layout of a bucket plan, argument checks.
+#pragma once
+#include "common.h"
+#include "../../include/cnnk_rel.h"
+
+// ---- generator -----------------------------------------------------------------------------------------------
+// Philox4x32 with seven rounds (J. Salmon, M. Moraes, R. Dror, D. Shaw, SC 2011), the fewest with which its authors found no
+// failing test.  A round is two 32 x 32 -> 64-bit products (v_mad_u64_u32).
+struct RelWords { unsigned w[4]; };
+struct RelKey { unsigned k0, k1; };
+__device__ __forceinline__ RelWords rel_words(unsigned c0, unsigned c1, unsigned c2, unsigned c3, RelKey k) {
+#pragma unroll
+  for (int i = 0; i < 7; ++i) {
+    const unsigned long long a = (unsigned long long)c0 * 0xD2511F53u, b = (unsigned long long)c2 * 0xCD9E8D57u;
+    c0 = (unsigned)(b >> 32) ^ c1 ^ k.k0;
+    c1 = (unsigned)b;
+    c2 = (unsigned)(a >> 32) ^ c3 ^ k.k1;
+    c3 = (unsigned)a;
+    k.k0 += 0x9E3779B9u;
+    k.k1 += 0xBB67AE85u;
+  }
+  return RelWords{{c0, c1, c2, c3}};
+}
+// the key of a call site in this step
+__device__ __forceinline__ RelKey rel_key(const unsigned long long* rng, unsigned site) {
+  const unsigned long long seed = rng[0], step = rng[1];
+  const RelWords r = rel_words((unsigned)step, (unsigned)(step >> 32), site, 0u, RelKey{(unsigned)seed, (unsigned)(seed >> 32)});
+  return RelKey{r.w[0], r.w[1]};
+}
+constexpr unsigned kDrawElements = 0, kDrawGroups = 1, kDrawPairs = 2;      // last word of the counter
+
+// p as a call takes it: elements whose 16-bit draw is below q are dropped, the others scaled by `scale`
+struct RelDrop { unsigned q; float scale; };
+static inline int rel_drop(float p, RelDrop* out) {
+  if (!(p >= 0.f && p < 1.f)) return CNNK_ERR_SHAPE;
+  out->q = (unsigned)((double)p * 65536.0 + 0.5);
+  if (out->q >= 65536u) return CNNK_ERR_UNSUPPORTED;
+  out->scale = (float)(65536.0 / (65536.0 - out->q));
+  return CNNK_OK;
+}
+
+static inline bool rel_aligned(const void* p, size_t a) { return ((size_t)p & (a - 1)) == 0; }
+
+// ---- bucket plan -----------------------------------------------------------------------------------------------
+// Pairs in 32 x 32 blocks, block (t / 32, u / 32) row by row, in a block 64 lanes of 16 in the order in which a wavefront holds the accumulator of
+// a 32 x 32 matrix product with one column a lane: lane (r / 4 % 2) * 32 + c, register (r / 8) * 4 + r % 4 for row r, column c.
+//   by_query  a lane a query (column), its registers keys    u16 [NT][NT][64][16]
+//   by_key    a lane a key, its registers queries, block (u / 32, t / 32)
+// An entry is 4 x bucket, the byte offset into a head's table in LDS; 4 x buckets for masked pairs and for padding, where that table holds -infinity.
+//   start     int [buckets + 1]: where a bucket's pairs begin in
+//   list      int [T * T]: places of its pairs in by_query, in the order of (t, u)
+constexpr int kRelMaxT = 8192, kRelMaxBuckets = 16382;
+struct RelPlan { size_t by_query, by_key, start, list, bytes; };
+static inline RelPlan rel_plan_layout(int T, int buckets) {
+  const size_t NT = (T + 31) / 32, map = align_up(NT * NT * 2048, 256);
+  RelPlan p;
+  p.by_query = 0;
+  p.by_key = map;
+  p.start = 2 * map;
+  p.list = p.start + align_up((size_t)(buckets + 1) * 4, 256);
+  p.bytes = p.list + align_up((size_t)T * T * 4, 256);
+  return p;
+}
+// place of row r, column c of a block in its 1024 entries
+__host__ __device__ __forceinline__ int rel_place(int r, int c) { return (((r >> 2 & 1) << 5 | c) << 4) | (r >> 3) << 2 | (r & 3); }

@@ -1,0 +1,375 @@
+"""GPU tests of include/cnnk_rel.h against oracle/rel.py in float64, with bounds from arithmetic: a stored bf16 value and every bf16 operand
+of a matrix product is off by at most eps / 2 = 2^-8 of itself, fp32 sums of n terms by n 2^-24 of the sum of their sizes."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import rel as R
+from util import host, rep
+
+pytestmark = pytest.mark.gpu
+
+HALF = {"bf16": 2.0 ** -8, "f32": 2.0 ** -24}
+DEV = "cuda:0"
+SEED, STEP, SITE = 0x9E3779B97F4A7C15, 5, 3
+
+
+@pytest.fixture(scope="module")
+def K():
+    assert torch.cuda.is_available(), "the GPU tests need a GPU"
+    from paper_2503_23186_amd import rel
+    return rel
+
+
+def typed(a, dtype):
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).to(DEV).to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+
+
+def state(seed=SEED, step=STEP):
+    return torch.from_numpy(np.array([seed, step], dtype=np.uint64).view(np.int64)).to(DEV)
+
+
+def stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def close(got, want, bound, what):
+    got = host(got) if torch.is_tensor(got) else got
+    assert np.isfinite(got).all(), "%s: not finite" % what
+    over = np.abs(got - want) - bound
+    assert (over <= 0).all(), "%s: off by %.3g where %.3g is allowed (at %s)" % (
+        what, np.abs(got - want).ravel()[over.argmax()], bound.ravel()[over.argmax()], np.unravel_index(over.argmax(), over.shape))
+
+
+# ---- dropout ---------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,C,p,span,bias,res", [(1, 8, 0.5, 0, True, True), (1, 8, 0.5, 1, False, False), (3, 24, 0.0, 0, True, False), (68, 128, 0.1, 0, True, True),
+                                                    (65, 264, 0.3, 0, False, True), (197, 768, 0.1, 0, True, True), (394, 768, 0.25, 197, False, True),
+                                                    (1000, 40, 0.9, 7, True, True), (2053, 1032, 0.1, 0, True, True), (50, 64, 0.2, 1000, True, True),
+                                                    (4099, 8, 0.15, 1, True, True), (130, 2048, 0.99998, 0, True, True)])
+def test_dropout(K, dtype, rows, C, p, span, bias, res):
+    rng = np.random.default_rng(rows + C)
+    z, r, dy = (rep(rng.standard_normal((rows, C)) + 0.01, dtype) for _ in range(3))
+    b = rep(0.5 * rng.standard_normal(C), "f32")
+    keep = R.keep_dropout(rows, C, p, span, R.site_key(SEED, STEP, SITE))
+    d = K.dropout_desc(rows, C, K.BF16 if dtype == "bf16" else K.F32, p, SITE, span)
+    gz, gr, gdy = typed(z, dtype), typed(r, dtype), typed(dy, dtype)
+    gb = typed(b, "f32") if bias else None
+    y, dz, db = torch.full_like(gz, 7.0), torch.full_like(gz, 7.0), torch.full((C,), 7.0, device=DEV)
+    s = state()
+    K.cnnk_dropout_fwd(d, gz, gb, gr if res else None, s, y)
+    want = keep * (z + (b if bias else 0.0)) + (r if res else 0.0)
+    size = np.abs(keep * (np.abs(z) + (np.abs(b) if bias else 0.0))) + (np.abs(r) if res else 0.0)
+    close(y, want, HALF[dtype] * np.abs(want) + 2.0 ** -21 * size, "y")
+    ws = torch.empty(max(256, K.cnnk_dropout_workspace_bytes(d)), dtype=torch.uint8, device=DEV)
+    K.cnnk_dropout_bwd(d, gdy, s, dz, db, ws, ws.numel())
+    wz = keep * dy
+    close(dz, wz, (HALF[dtype] + 2.0 ** -22) * np.abs(wz), "dz")
+    assert ((host(dz) == 0) == (keep == 0)).all()                # the same draws, element by element
+    close(db, wz.sum(0), (rows + 8) * 2.0 ** -24 * np.abs(wz).sum(0) + 1e-30, "dbias")
+    alone = torch.full_like(gz, 7.0)
+    K.cnnk_dropout_bwd(d, gdy, s, alone)                          # without the sums
+    assert torch.equal(alone, dz)
+    again = torch.full((C,), 3.0, device=DEV)
+    K.cnnk_dropout_bwd(d, gdy, s, gdy, again, ws, ws.numel())     # in place, the same bits
+    assert torch.equal(gdy, dz) and torch.equal(again, db)
+    K.cnnk_dropout_fwd(d, gz, gb, gr if res else None, s, gz)     # y over z
+    assert torch.equal(gz, y)
+
+
+def test_dropout_writes_its_rows_only(K):
+    rows, C = 37, 40
+    full = torch.full((rows + 2, C), 5.0, device=DEV, dtype=torch.bfloat16)
+    z = torch.ones(rows, C, device=DEV, dtype=torch.bfloat16)
+    d = K.dropout_desc(rows, C, K.BF16, 0.4, SITE)
+    K.cnnk_dropout_fwd(d, z, None, None, state(), full[1])
+    assert (full[0] == 5).all() and (full[-1] == 5).all()
+
+
+def test_dropout_of_a_tensor_past_4_gib(K):
+    """2.15e9 bf16 values: byte offsets pass 32 bits.  The last rows against the oracle's draws at their own places."""
+    rows, C, p = 268436, 8192, 0.3
+    z = torch.ones(rows, C, device=DEV, dtype=torch.bfloat16)
+    K.cnnk_dropout_fwd(K.dropout_desc(rows, C, K.BF16, p, SITE), z, None, None, state(), z)
+    n = 4 * C
+    first = rows * C - n
+    i = (first + np.arange(n, dtype=np.uint64)) // np.uint64(8)
+    zero = np.zeros_like(i)
+    words = R.philox((i & R.LOW, i >> np.uint64(32), zero, zero), R.site_key(SEED, STEP, SITE))
+    draw = R.pieces(words)[np.arange(n), (first + np.arange(n)) % 8]
+    q, f = R.share(p)
+    got = z[-4:].float().cpu().numpy().ravel()
+    assert ((got != 0) == (draw >= q)).all() and abs(got.max() - f) <= f * 2.0 ** -8
+    kept = float((z != 0).sum(dtype=torch.int64)) / z.numel()
+    assert abs(kept - (1 - q / 65536)) < 6 * np.sqrt(p / z.numel())
+
+
+def test_steps_and_sites_in_a_captured_graph(K):
+    """The state moves on inside of the graph: every replay draws as the eager call of its step does."""
+    rows, C, p = 50, 64, 0.5
+    z = torch.ones(rows, C, device=DEV)
+    s, y = state(step=2 ** 32 - 2), torch.zeros_like(z)
+    d = [K.dropout_desc(rows, C, K.F32, p, site) for site in (0, 1)]
+    side = torch.cuda.Stream()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        K.cnnk_dropout_fwd(d[0], z, None, None, s, y, stream())
+        K.cnnk_dropout_fwd(d[1], y, None, None, s, y, stream())
+        K.cnnk_rng_advance(s, 1, stream())
+    for k in range(4):
+        want = np.ones((rows, C))
+        for site in (0, 1):
+            want = want * R.keep_dropout(rows, C, p, 0, R.site_key(SEED, 2 ** 32 - 2 + k, site))
+        g.replay()
+        torch.cuda.synchronize()
+        assert (host(y) == want).all(), k
+        (z * 2).sum().item()
+    assert s.cpu().numpy().view(np.uint64).tolist() == [SEED, 2 ** 32 + 2]
+
+
+# ---- buckets -----------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("gh,gw,cls", [(1, 1, 0), (1, 1, 1), (4, 4, 1), (3, 7, 0), (14, 14, 1), (1, 33, 1), (24, 20, 1)])
+def test_grid_buckets(K, gh, gw, cls):
+    T = gh * gw + cls
+    m = torch.full((T, T), -7, dtype=torch.int32, device=DEV)
+    K.cnnk_rel_buckets_grid(gh, gw, cls, m)
+    want = R.grid_buckets(gh, gw, cls)
+    assert (m.cpu().numpy() == want).all() and want.max() < K.grid_buckets(gh, gw, cls)
+
+
+def test_plans_are_reproducible_and_ignore_what_they_overwrite(K):
+    T, n = 197, 30
+    m = torch.from_numpy(np.random.default_rng(1).integers(-2, n + 2, (T, T)).astype(np.int32)).to(DEV)
+    a = torch.full((K.cnnk_rel_plan_bytes(T, n),), 255, dtype=torch.uint8, device=DEV)
+    b = torch.zeros_like(a)
+    for p, fill in ((a, 255), (b, 0)):
+        ws = torch.full((K.cnnk_rel_plan_workspace_bytes(T, n),), fill, dtype=torch.uint8, device=DEV)
+        K.cnnk_rel_plan(T, n, m, p, ws, ws.numel())
+    NT = (T + 31) // 32
+    maps = 2 * NT * NT * 2048                                    # then the starts and the lists
+    start = a[maps:maps + 4 * (n + 1)].view(torch.int32).cpu().numpy()
+    ids = m.cpu().numpy().ravel()
+    want = np.concatenate([[0], np.cumsum([(ids == k).sum() for k in range(n)])])
+    assert (start == want).all()
+    at = maps + (4 * (n + 1) + 255) // 256 * 256
+    lists = [x[at:at + 4 * int(start[-1])].view(torch.int32) for x in (a, b)]
+    assert torch.equal(lists[0], lists[1]) and torch.equal(a[:maps], b[:maps])
+    order = lists[0].cpu().numpy()
+    block, place = order >> 10, order & 1023
+    lane, reg = place >> 4, place & 15
+    t, u = block // NT * 32 + (lane & 31), block % NT * 32 + (reg >> 2) * 8 + (lane >> 5) * 4 + (reg & 3)
+    assert (t * T + u == np.concatenate([np.flatnonzero(ids == k) for k in range(n)])).all()
+
+
+# ---- attention ---------------------------------------------------------------------------------------------------------------
+
+class Case:
+    """Inputs, the oracle's results and the library's of one attention call."""
+
+    def __init__(self, K, dtype, B, T, heads, dh, bucket, n, p, lens=None, table=None, seed=0, scale=1.0, past=0.0, d_o=None):
+        self.K, self.dtype, self.B, self.T, self.heads, self.dh, self.n = K, dtype, B, T, heads, dh, n
+        rng = np.random.default_rng(seed + 7919 * T + dh)
+        self.qkv = rep(scale * rng.standard_normal((B, T, 3 * heads * dh)), dtype)
+        self.g = rep(0.3 * rng.standard_normal((B, T, heads * dh)), dtype) if d_o is None else d_o
+        self.table = None if n == 0 else rep(0.7 * rng.standard_normal((n, heads)), "f32") if table is None else table
+        self.bucket, self.lens, self.p = bucket if n else None, lens, p
+        self.keep = R.keep_pairs(B, heads, T, p, R.site_key(SEED, STEP, SITE)) if p else None
+        self.ref = R.attention(self.qkv, heads, self.table, self.bucket, lens, self.keep, self.g)
+        qkv, g = self.qkv.copy(), self.g.copy()
+        if lens is not None and past is not None:
+            for b, m in enumerate(lens):
+                qkv[b, max(0, m):], g[b, max(0, m):] = past, past
+        self.gq, self.gg = typed(qkv, dtype), typed(g, dtype)
+        self.gt = None if n == 0 else typed(self.table, "f32")
+        self.plan = None if n == 0 else K.make_plan(torch.from_numpy(np.ascontiguousarray(bucket, dtype=np.int32)).to(DEV), n)
+        self.gl = None if lens is None else torch.tensor(lens, dtype=torch.int32, device=DEV)
+        self.desc = K.rel_desc(B, T, heads, dh, K.BF16 if dtype == "bf16" else K.F32, n, p, SITE)
+        self.s = state()
+
+    def fwd(self, rest=True, stats=True, st=None):
+        o = torch.full((self.B, self.T, self.heads * self.dh), 9.0, device=DEV, dtype=self.gq.dtype)
+        r = torch.full_like(o, 9.0) if rest and self.dtype == "bf16" else None
+        m = torch.full((self.B, self.heads, self.T, 2), 9.0, device=DEV) if stats else None
+        self.K.cnnk_rel_attention_fwd(self.desc, self.gq, self.gt, self.plan, self.gl, self.s if self.p else None, o, r, m, stream() if st is None else st)
+        return o, r, m
+
+    def bwd(self, o, r, m, table=True, st=None):
+        dq = torch.full_like(self.gq, 9.0)
+        dt = torch.full((self.n, self.heads), 9.0, device=DEV) if table and self.n else None
+        ws = torch.full((self.K.cnnk_rel_attention_workspace_bytes(self.desc),), 255, dtype=torch.uint8, device=DEV)
+        self.K.cnnk_rel_attention_bwd(self.desc, self.gq, o, r, self.gg, self.gt, self.plan, self.gl, self.s if self.p else None, m, dq, dt, ws, ws.numel(),
+                                      stream() if st is None else st)
+        return dq, dt
+
+    def slack(self):
+        """Relative error of a probability or of dx's terms from fp32: scores of dh terms, sums of T terms, two exponentials and what is around them."""
+        size = float(self.ref["scores"].max()) + (float(np.abs(self.table[self.table > -1e30]).max()) if self.n and (self.table > -1e30).any() else 0.0)
+        return 2.0 * ((self.dh + 16) * 2.0 ** -24 * size + (self.T + 64) * 2.0 ** -24 + 2.0 ** -21)
+
+    def check(self, rest=True):
+        ref, e, h = self.ref, self.slack(), HALF[self.dtype]
+        a = h if self.dtype == "bf16" else 0.0                     # operands of the second products
+        o, r, m = self.fwd(rest=rest)
+        close(o, ref["o"], h * np.abs(ref["o"]) + (a + e) * ref["bound_o"] * 1.01 + 1e-30, "o")
+        top, log = host(m[..., 0]), host(m[..., 1])
+        none = np.isneginf(ref["top"])
+        assert (np.isneginf(top) == none).all() and (log[none] == 0).all()
+        both = np.where(none, 0.0, np.where(none, 0.0, top) + log)
+        want = np.where(none, 0.0, np.where(none, 0.0, ref["top"]) + ref["log"])
+        close(both, want, e * (1 + np.abs(want)) + 2.0 ** -23 * np.abs(np.where(none, 0.0, ref["top"])), "statistics")
+        dq, dt = self.bwd(o, r, m)
+        # delta = do . o, with o and what was taken off it 2^-16 of o off, as stored alone 2^-8
+        d = 0.0 if self.dtype == "f32" else 2.0 ** -16 if rest else 2.0 ** -8
+        close(dq, ref["dqkv"], h * np.abs(ref["dqkv"]) + a * 1.01 * ref["bound_dqkv"] + (e + d) * ref["size_dqkv"] * 1.01 + 1e-30, "dqkv")
+        if self.n:
+            close(dt, ref["dtable"], (e + d) * ref["size_dtable"] * 1.01 + 2.0 ** -23 * np.abs(ref["dtable"]) + 1e-30, "dtable")
+        return o, r, m, dq, dt
+
+
+def map_of(kind, T, seed=0):
+    """(map, buckets): 'grid' with a class token where T allows, 'none', 'one' bucket for all, 'random' with masked pairs, rows and keys that see nothing."""
+    rng = np.random.default_rng(seed + T)
+    if kind == "none":
+        return None, 0
+    if kind == "one":
+        return np.zeros((T, T), dtype=np.int32), 1
+    if kind == "grid":
+        side = int(np.sqrt(max(1, T - 1)))
+        while T > 1 and (T - 1) % side:
+            side -= 1
+        gh, gw, cls = (side, (T - 1) // side, 1) if T > 1 else (1, 1, 0)
+        return R.grid_buckets(gh, gw, cls), (2 * gh - 1) * (2 * gw - 1) + 3 * cls
+    n = 37
+    m = rng.integers(-8, n + 5, (T, T)).astype(np.int32)            # outside 0 .. 36: masked
+    m[m == 11] = 12                                                 # a bucket without pairs
+    m[rng.integers(0, T)] = -1
+    m[:, rng.integers(0, T)] = n + 3
+    return m, n
+
+
+SHAPES = [(1, 1, 1, 64), (2, 2, 3, 16), (3, 17, 2, 64), (1, 31, 2, 32), (2, 32, 1, 128), (2, 33, 3, 64), (1, 65, 2, 16), (2, 64, 2, 64), (1, 130, 2, 128), (2, 197, 3, 64),
+          (5, 50, 1, 32), (1, 260, 2, 64), (1, 321, 1, 32)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind,p", [("none", 0.0), ("grid", 0.0), ("grid", 0.1), ("random", 0.3), ("none", 0.5), ("one", 0.0)])
+@pytest.mark.parametrize("B,T,heads,dh", SHAPES)
+def test_attention(K, dtype, B, T, heads, dh, kind, p):
+    bucket, n = map_of(kind, T)
+    Case(K, dtype, B, T, heads, dh, bucket, n, p).check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind,p", [("none", 0.0), ("grid", 0.2), ("random", 0.1)])
+@pytest.mark.parametrize("T,heads,dh,lens", [(40, 2, 64, [0, 1, 40, 33, -5, 99]), (197, 1, 64, [197, 5, 96, 128]), (70, 2, 32, [64, 65, 0, 31]), (33, 1, 128, [32, 33]),
+                                             (150, 2, 16, [0, 0, 149])])
+def test_padded_batches(K, dtype, kind, p, T, heads, dh, lens):
+    """What lies past an image's tokens is of no account: not a number there."""
+    bucket, n = map_of(kind, T)
+    Case(K, dtype, len(lens), T, heads, dh, bucket, n, p, lens=lens, past=np.nan).check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_larger_attention(K, dtype):
+    bucket, n = map_of("grid", 577)
+    Case(K, dtype, 2, 577, 2, 64, bucket, n, 0.1, lens=[577, 400]).check()
+
+
+@pytest.mark.parametrize("T,dh", [(197, 64), (65, 128), (40, 16)])
+def test_output_without_its_rest(K, T, dh):
+    bucket, n = map_of("grid", T)
+    Case(K, "bf16", 2, T, 2, dh, bucket, n, 0.1).check(rest=False)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [20, 100])
+def test_scores_of_every_size(K, dtype, T):
+    """Tables with -infinity (masks), with the lowest finite value for whole rows (shared out evenly) and beside others (nothing left), and scores of some hundreds."""
+    n, heads, low = 6, 2, float(np.finfo(np.float32).min)
+    bucket = np.random.default_rng(3).integers(0, 3, (T, T)).astype(np.int32)
+    bucket[1] = 3                        # a row of the lowest value
+    bucket[2] = 4                        # a row of -infinity
+    bucket[3, ::2] = 4
+    bucket[4, ::3] = 3
+    bucket[5] = np.where(np.arange(T) == T - 1, 5, 3)
+    table = np.zeros((n, heads))
+    table[:3] = np.random.default_rng(4).standard_normal((3, heads)).astype(np.float32)
+    table[3], table[4], table[5] = low, -np.inf, 2.0
+    c = Case(K, dtype, 2, T, heads, 64, bucket, n, 0.0, table=table)
+    o, r, m, dq, dt = c.check()
+    v = c.qkv.reshape(2, T, 3, heads, 64)[:, :, 2]
+    assert np.abs(host(o)[:, 1].reshape(2, heads, 64) - v.mean(1)).max() < 2.0 ** -7 * np.abs(v).mean(1).max()
+    assert (host(o)[:, 2] == 0).all() and (host(dt)[4] == 0).all()
+    bucket, n = map_of("one", T)
+    Case(K, dtype, 1, T, 2, 64, bucket, n, 0.0, scale=8.0).check()
+    Case(K, dtype, 1, T, 2, 64, bucket, n, 0.0, table=np.full((1, 2), -1e6)).check()
+    Case(K, dtype, 1, T, 2, 64, None, 0, 0.0, scale=1e-3).check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,dh", [(130, 64), (40, 32), (197, 128)])
+def test_same_bits_again_and_on_another_stream(K, dtype, T, dh):
+    bucket, n = map_of("random", T)
+    c = Case(K, dtype, 3, T, 2, dh, bucket, n, 0.2, lens=[T, T - 3, 7])
+    o, r, m = c.fwd()
+    dq, dt = c.bwd(o, r, m)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        o2, r2, m2 = c.fwd()
+        dq2, dt2 = c.bwd(o2, r2, m2)
+    side.synchronize()
+    for a, b in ((o, o2), (r, r2), (m, m2), (dq, dq2), (dt, dt2)):
+        assert a is None or torch.equal(a, b)
+    o3, _, _ = c.fwd(rest=False, stats=False)                      # evaluation
+    assert torch.equal(o3, o)
+    dq3, _ = c.bwd(o, r, m, table=False)                           # a table that is not learned
+    assert torch.equal(dq3, dq)
+
+
+def test_nothing_past_the_outputs_is_written(K):
+    B, T, heads, dh = 2, 45, 2, 32
+    bucket, n = map_of("grid", T)
+    c = Case(K, "bf16", B, T, heads, dh, bucket, n, 0.1)
+    guard = lambda shape, dt: torch.full((int(np.prod(shape)) + 512,), 3.0, dtype=dt, device=DEV)
+    o, r, dq = (guard((B, T, k * heads * dh), torch.bfloat16) for k in (1, 1, 3))
+    m, dt = guard((B, heads, T, 2), torch.float32), guard((n, heads), torch.float32)
+    need = K.cnnk_rel_attention_workspace_bytes(c.desc)
+    ws = torch.full((need + 1024,), 77, dtype=torch.uint8, device=DEV)
+    at = lambda t: t.data_ptr() + 256 * t.element_size()
+    K.cnnk_rel_attention_fwd(c.desc, c.gq, c.gt, c.plan, None, c.s, at(o), at(r), at(m))
+    K.cnnk_rel_attention_bwd(c.desc, c.gq, at(o), at(r), c.gg, c.gt, c.plan, None, c.s, at(m), at(dq), at(dt), ws.data_ptr() + 256, need)
+    torch.cuda.synchronize()
+    for t, k in ((o, 1), (r, 1), (dq, 3)):
+        assert (t[:256] == 3).all() and (t[256 + B * T * k * heads * dh:] == 3).all()
+    assert (m[:256] == 3).all() and (m[256 + B * heads * T * 2:] == 3).all() and (dt[:256] == 3).all() and (dt[256 + n * heads:] == 3).all()
+    assert (ws[:256] == 77).all() and (ws[256 + need:] == 77).all()
+
+
+def test_an_image_far_behind_in_a_large_batch(K):
+    """Byte offsets past 32 bits: the last image of 4.4 GB of qkv gives what it gives alone."""
+    B, T, heads, dh = 2400, 400, 12, 64
+    n = K.grid_buckets(20, 20, 0)
+    m = torch.empty(T, T, dtype=torch.int32, device=DEV)
+    K.cnnk_rel_buckets_grid(20, 20, 0, m)
+    plan = K.make_plan(m, n)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    one, table = torch.randn(1, T, 3 * heads * dh, generator=g, device=DEV).bfloat16(), torch.randn(n, heads, generator=g, device=DEV)
+    d_o = torch.randn(1, T, heads * dh, generator=g, device=DEV).bfloat16()
+    out = []
+    for b in (1, B):
+        qkv, go = torch.zeros(b, T, 3 * heads * dh, dtype=torch.bfloat16, device=DEV), torch.zeros(b, T, heads * dh, dtype=torch.bfloat16, device=DEV)
+        qkv[-1], go[-1] = one[0], d_o[0]
+        lens = torch.zeros(b, dtype=torch.int32, device=DEV)
+        lens[-1] = T
+        desc = K.rel_desc(b, T, heads, dh, K.BF16, n, 0.0, 0)
+        o, st = torch.empty_like(go), torch.empty(b, heads, T, 2, device=DEV)
+        K.cnnk_rel_attention_fwd(desc, qkv, table, plan, lens, None, o, None, st, stream())
+        dq, dt = torch.empty_like(qkv), torch.empty_like(table)
+        ws = torch.empty(K.cnnk_rel_attention_workspace_bytes(desc), dtype=torch.uint8, device=DEV)
+        K.cnnk_rel_attention_bwd(desc, qkv, o, None, go, table, plan, lens, None, st, dq, dt, ws, ws.numel(), stream())
+        out.append((o[-1].clone(), dq[-1].clone(), dt, bool((o[:-1] == 0).all()) and bool((dq[:-1] == 0).all())))
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1]) and out[1][3]
+    assert torch.allclose(out[0][2], out[1][2], rtol=1e-5, atol=1e-6)
