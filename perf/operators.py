@@ -134,9 +134,8 @@ def prepare(case, seed):
             s["plan"] = buf(rel.cnnk_rel_plan_bytes(T, n))
             ws = buf(rel.cnnk_rel_plan_workspace_bytes(T, n))
             rel.cnnk_rel_plan(T, n, s["map"], s["plan"], ws, ws.numel(), stream)
-            s["o"], s["o_rest"] = torch.empty(B, T, H * dh, dtype=t, device=DEV), None
+            s["o"] = torch.empty(B, T, H * dh, dtype=t, device=DEV)
             if case["train"]:
-                s["o_rest"] = torch.empty_like(s["o"]) if case["dtype"] == "bf16" else None
                 s["stats"] = torch.empty(B, H, T, 2, device=DEV)
                 s["dqkv"], s["dtable"] = torch.empty_like(s["qkv"]), torch.empty_like(s["table"])
                 s["ws"] = buf(rel.cnnk_rel_attention_workspace_bytes(s["desc"]))
@@ -160,10 +159,10 @@ def run_own(s):
         rel.cnnk_dropout_bwd(s["desc"], s["dy"], s["rng"], s["dz"], db, s["ws"], s["ws"].numel(), stream)
         return [s["y"], s["dz"]] + ([db] if s["bias"] else [])
     if not s["train"]:
-        rel.cnnk_rel_attention_fwd(s["desc"], s["qkv"], s["table"], s["plan"], s["lens"], s["rng"], s["o"], None, None, stream)
+        rel.cnnk_rel_attention_fwd(s["desc"], s["qkv"], s["table"], s["plan"], s["lens"], s["rng"], s["o"], None, stream)
         return s["o"]
-    rel.cnnk_rel_attention_fwd(s["desc"], s["qkv"], s["table"], s["plan"], s["lens"], s["rng"], s["o"], s["o_rest"], s["stats"], stream)
-    rel.cnnk_rel_attention_bwd(s["desc"], s["qkv"], s["o"], s["o_rest"], s["d_o"], s["table"], s["plan"], s["lens"], s["rng"], s["stats"], s["dqkv"],
+    rel.cnnk_rel_attention_fwd(s["desc"], s["qkv"], s["table"], s["plan"], s["lens"], s["rng"], s["o"], s["stats"], stream)
+    rel.cnnk_rel_attention_bwd(s["desc"], s["qkv"], s["o"], s["d_o"], s["table"], s["plan"], s["lens"], s["rng"], s["stats"], s["dqkv"],
                                s["dtable"], s["ws"], s["ws"].numel(), stream)
     return [s["o"], s["dqkv"], s["dtable"]]
 
