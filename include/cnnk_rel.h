@@ -68,17 +68,17 @@ int cnnk_rel_plan(int T, int buckets, const int* bucket, void* plan, void* ws, s
  * masked pairs are computed and left out.
  * table [buckets][heads] float; buckets = 0: no bias, table and plan are not read.
  * Dropout: query t, key u of (image b, head h) has half u % 2 of word t % 4 of F(u / 2, t / 4, b * heads + h, 2).
- * Training: stats [B][heads][T][2] receives each row's largest x and the logarithm of sum_u exp(x - largest) (a row that sees no key: -infinity and 0);
- * o_rest [B][T][heads * dh] (bf16 storage only, otherwise not used) receives what rounding took off o, so that the backward pass has the sum of both. Both may be
- * NULL in evaluation; without o_rest the backward pass takes o as stored: dtable is then about 1e-4 of its norm off instead of 1e-6.
- * dh in {16, 32, 64, 128}; T <= 16384, 8192 with buckets; the elements of an image's qkv take less than 2^31 bytes. */
+ * Training: stats [B][heads][T][2] receives a reference near each row's largest x and the logarithm of
+ * sum_u exp(x - reference) (a row that sees no key: -infinity and 0);
+ * NULL in evaluation.
+ * dh in {16, 32, 64, 128}; T <= 16384, 8192 with buckets; heads <= 65535; the elements of an image's qkv take less than 2^31 bytes. */
 typedef struct { int B, T, heads, dh; int dtype; int buckets; float p; unsigned site; } cnnk_rel_desc;
 int cnnk_rel_attention_fwd(const cnnk_rel_desc* d, const void* qkv, const float* table, const void* plan, const int* lens,
-                           const unsigned long long* rng, void* o, void* o_rest, float* stats, void* stream);
+                           const unsigned long long* rng, void* o, float* stats, void* stream);
 
-/* dqkv (all of it: zeros past an image's tokens) and dtable [buckets][heads] (overwritten; NULL: not formed).  o, o_rest, stats: as the forward call left them, with the same lens, rng and plan. */
+/* dqkv (all of it: zeros past an image's tokens) and dtable [buckets][heads] (overwritten; NULL: not formed).  o, stats: as the forward call left them, with the same lens, rng and plan. */
 size_t cnnk_rel_attention_workspace_bytes(const cnnk_rel_desc* d);              
-int cnnk_rel_attention_bwd(const cnnk_rel_desc* d, const void* qkv, const void* o, const void* o_rest, const void* d_o,
+int cnnk_rel_attention_bwd(const cnnk_rel_desc* d, const void* qkv, const void* o, const void* d_o,
                            const float* table, const void* plan, const int* lens, const unsigned long long* rng,
                            const float* stats, void* dqkv, float* dtable, void* ws, size_t ws_bytes, void* stream);
 

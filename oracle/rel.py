@@ -114,7 +114,7 @@ def attention(qkv, heads, table=None, bucket=None, lens=None, keep=None, d_o=Non
     vt = v.transpose(0, 1, 3, 2)
     dP = (g @ vt) * keep
     dx = P * (dP - (P * dP).sum(-1, keepdims=True))
-    size = P * (keep * (np.abs(g) @ np.abs(vt)) + (np.abs(g) * np.abs(O)).sum(-1, keepdims=True))      # of the terms of dx
+    size = P * (keep * (np.abs(g) @ np.abs(vt)) + (np.abs(g) * (D @ np.abs(v))).sum(-1, keepdims=True))      # of the terms of dx, delta's among them
     t = lambda a: a.transpose(0, 1, 3, 2)
     three = lambda a, b, c: np.stack([z.transpose(0, 2, 1, 3) for z in (a, b, c)], 2).reshape(B, T, 3 * heads * dh)
     r["dqkv"] = three(dx @ k * s, t(dx) @ q * s, t(D) @ g)

@@ -76,6 +76,14 @@ __device__ __forceinline__ void load16_to_lds(i32x4_t desc, unsigned lds_addr, u
                : "s"(lds_addr), "v"(voff), "s"(desc)
                : "memory");
 }
+// the same with 4 bytes a lane
+__device__ __forceinline__ void load4_to_lds(i32x4_t desc, unsigned lds_addr, unsigned voff) {
+  unsigned keep;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dword %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+               : "=&s"(keep)
+               : "s"(lds_addr), "v"(voff), "s"(desc)
+               : "memory");
+}
 // What the index of a 16-byte chunk is XORed with to give its position in the LDS row.  64-byte rows
 // read with 16-byte loads: row bits 2-3; read with the transposing load: nothing, four consecutive
 // rows are the 64 banks whatever the order inside a row.

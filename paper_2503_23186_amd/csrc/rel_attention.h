@@ -1,0 +1,25 @@
+// What the attention kernels behind include/cnnk_rel.h get: the general ones (rel_attention.hip) and those on the matrix cores (rel_attention_mfma.hip).
+#pragma once
+#include "rel.h"
+
+struct RelArgs {
+  int B, T, Tp, heads, dh, NT, buckets;      // Tp: T rounded up to 64, NT: blocks of 32
+  float scale;                               // 1 / sqrt(dh)
+  unsigned site;
+  RelDrop dr;
+  const float* table;
+  const unsigned short *by_query, *by_key;
+  const int *start, *list, *lens;
+  const unsigned long long* rng;
+};
+// tokens of image b
+__device__ __forceinline__ int rel_tokens(const RelArgs& a, int b) {
+  if (!a.lens) return a.T;
+  const int n = a.lens[b];
+  return n < 0 ? 0 : n > a.T ? a.T : n;
+}
+
+// bf16 storage.  rows: [B * heads][3][Tp] floats, pairs (NULL: no gradient of the table): [splits][heads][NT][NT][1024]
+int rel_mfma_fwd(const RelArgs& a, const void* qkv, void* o, float* stats, hipStream_t st);
+int rel_mfma_bwd(const RelArgs& a, const void* qkv, const void* o, const void* d_o, const float* stats, void* dqkv, float* rows, float* pairs, int splits,
+                 hipStream_t st);

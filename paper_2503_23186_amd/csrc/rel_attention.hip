@@ -1,24 +1,13 @@
-// Self-attention with a learned relative position bias, dropout of the probabilities and padded batches (include/cnnk_rel.h): the general
-// kernels, one wavefront to a row of scores.
+// Self-attention with a learned relative position bias, dropout of the probabilities and padded batches (include/cnnk_rel.h): the kernels
+// of fp32 storage, one wavefront to a row of scores (bf16: rel_attention_mfma.hip), and the entry points.
 //
 // Scores of 64 keys (queries) at a time, one a lane; the products with V, K, Q and dO that follow go over the same 64 with a feature a lane,
 // the factors from LDS.  Probabilities are not stored: the forward pass keeps a row's largest score and the logarithm of its sum, apart, so that
-// scores near the lowest finite value lose nothing.  dx = P (dP - delta), delta = do . o, where o is what was stored plus what rounding took off.
-#include "rel.h"
+// scores near the lowest finite value lose nothing.  dx = P (dP - delta), delta = do . o.
+#include "rel_attention.h"
 
 namespace {
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
-
-struct Args {
-  int B, T, heads, dh, NT, buckets;
-  float scale;                 // 1 / sqrt(dh)
-  unsigned site;
-  RelDrop dr;
-  const float* table;
-  const unsigned short* by_query;
-  const int *start, *list, *lens;
-  const unsigned long long* rng;
-};
 
 template <typename T> __device__ __forceinline__ float dot_rows(const T* a, const T* b, int dh) {
   float s = 0.f;
@@ -32,22 +21,17 @@ template <typename T> __device__ __forceinline__ float dot_rows(const T* a, cons
   return s;
 }
 // score of query t, key u, both within the image: -infinity if masked
-__device__ __forceinline__ float score(const Args& a, float qk, int t, int u, int h) {
+__device__ __forceinline__ float score(const RelArgs& a, float qk, int t, int u, int h) {
   if (!a.buckets) return qk * a.scale;
   const int k = a.by_query[((size_t)(t >> 5) * a.NT + (u >> 5)) * 1024 + rel_place(u & 31, t & 31)] >> 2;
   return k < a.buckets ? fmaf(qk, a.scale, a.table[(size_t)k * a.heads + h]) : -INFINITY;
 }
-__device__ __forceinline__ float keep(const Args& a, RelKey key, int bh, int t, int u) {      // 1 / (1 - p) or 0
+__device__ __forceinline__ float keep(const RelArgs& a, RelKey key, int bh, int t, int u) {      // 1 / (1 - p) or 0
   if (!a.dr.q) return 1.f;
   const RelWords r = rel_words((unsigned)u >> 1, (unsigned)t >> 2, (unsigned)bh, kDrawPairs, key);
   const int i = t & 3;
   const unsigned w = i < 2 ? (i ? r.w[1] : r.w[0]) : (i == 2 ? r.w[2] : r.w[3]);
   return (u & 1 ? w >> 16 : w & 0xffffu) < a.dr.q ? 0.f : a.dr.scale;
-}
-__device__ __forceinline__ int tokens(const Args& a, int b) {
-  if (!a.lens) return a.T;
-  const int n = a.lens[b];
-  return n < 0 ? 0 : n > a.T ? a.T : n;
 }
 // sum over 64 rows from `row0` (at most n) of f[j] * m[row][c], for this lane's features lane and lane + 64
 template <typename T> __device__ __forceinline__ void add_rows(const float* f, const T* m, size_t ld, int row0, int n, int dh, int lane, float acc[2]) {
@@ -61,9 +45,9 @@ template <typename T> __device__ __forceinline__ void add_rows(const float* f, c
 }
 
 template <typename T>
-__global__ void __launch_bounds__(64) rel_fwd_kernel(Args a, const T* __restrict__ qkv, T* __restrict__ o, T* __restrict__ o_rest, float* __restrict__ stats) {
+__global__ void __launch_bounds__(64) rel_fwd_kernel(RelArgs a, const T* __restrict__ qkv, T* __restrict__ o, float* __restrict__ stats) {
   __shared__ float f[64];
-  const int bh = blockIdx.y, b = bh / a.heads, h = bh - b * a.heads, t = blockIdx.x, lane = threadIdx.x, d = a.heads * a.dh, n = tokens(a, b);
+  const int bh = blockIdx.x / a.T, b = bh / a.heads, h = bh - b * a.heads, t = blockIdx.x - bh * a.T, lane = threadIdx.x, d = a.heads * a.dh, n = rel_tokens(a, b);
   const size_t ld = 3 * (size_t)d;
   const T* base = qkv + (size_t)b * a.T * ld + h * a.dh;
   float m = -INFINITY, l = 0.f, acc[2] = {0.f, 0.f};
@@ -94,7 +78,6 @@ __global__ void __launch_bounds__(64) rel_fwd_kernel(Args a, const T* __restrict
     const float v = t < n ? acc[i] * inv : 0.f;
     const size_t at = ((size_t)b * a.T + t) * d + h * a.dh + c;
     Elem<T>::st(o + at, v);
-    if (sizeof(T) == 2 && o_rest) Elem<T>::st(o_rest + at, v - Elem<T>::ld(o + at));
   }
   if (stats && lane == 0) {
     float* s = stats + ((size_t)bh * a.T + t) * 2;
@@ -105,14 +88,14 @@ __global__ void __launch_bounds__(64) rel_fwd_kernel(Args a, const T* __restrict
 
 // delta of every row: a wavefront to four rows, 16 lanes to one
 template <typename T>
-__global__ void __launch_bounds__(256) rel_delta_kernel(Args a, const T* __restrict__ o, const T* __restrict__ o_rest, const T* __restrict__ d_o, float* __restrict__ delta) {
+__global__ void __launch_bounds__(256) rel_delta_kernel(RelArgs a, const T* __restrict__ o, const T* __restrict__ d_o, float* __restrict__ delta) {
   const size_t row = (size_t)blockIdx.x * 16 + (threadIdx.x >> 4);      // (b * heads + h) * T + t
   if (row >= (size_t)a.B * a.heads * a.T) return;
   const int t = (int)(row % (unsigned)a.T), bh = (int)(row / (unsigned)a.T), b = bh / a.heads, h = bh - b * a.heads;
   const size_t at = ((size_t)b * a.T + t) * a.heads * a.dh + h * a.dh;
   float s = 0.f;
   for (int c = threadIdx.x & 15; c < a.dh; c += 16)
-    s = fmaf(Elem<T>::ld(d_o + at + c), Elem<T>::ld(o + at + c) + (o_rest ? Elem<T>::ld(o_rest + at + c) : 0.f), s);
+    s = fmaf(Elem<T>::ld(d_o + at + c), Elem<T>::ld(o + at + c), s);
   s += row_rotated<8>(s);
   s += row_rotated<4>(s);
   s += row_rotated<2>(s);
@@ -124,10 +107,10 @@ __global__ void __launch_bounds__(256) rel_delta_kernel(Args a, const T* __restr
 __device__ __forceinline__ float prob(float x, const float* st) { return st[0] > -INFINITY ? __builtin_amdgcn_exp2f((x - st[0] - st[1]) * kLog2e) : 0.f; }
 
 template <typename T>
-__global__ void __launch_bounds__(64) rel_dq_kernel(Args a, const T* __restrict__ qkv, const T* __restrict__ d_o, const float* __restrict__ stats,
+__global__ void __launch_bounds__(64) rel_dq_kernel(RelArgs a, const T* __restrict__ qkv, const T* __restrict__ d_o, const float* __restrict__ stats,
                                                     const float* __restrict__ delta, T* __restrict__ dqkv) {
   __shared__ float f[64];
-  const int bh = blockIdx.y, b = bh / a.heads, h = bh - b * a.heads, t = blockIdx.x, lane = threadIdx.x, d = a.heads * a.dh, n = tokens(a, b);
+  const int bh = blockIdx.x / a.T, b = bh / a.heads, h = bh - b * a.heads, t = blockIdx.x - bh * a.T, lane = threadIdx.x, d = a.heads * a.dh, n = rel_tokens(a, b);
   const size_t ld = 3 * (size_t)d;
   const T *base = qkv + (size_t)b * a.T * ld + h * a.dh, *g = d_o + ((size_t)b * a.T + t) * d + h * a.dh;
   float acc[2] = {0.f, 0.f};
@@ -155,10 +138,10 @@ __global__ void __launch_bounds__(64) rel_dq_kernel(Args a, const T* __restrict_
 }
 
 template <typename T>
-__global__ void __launch_bounds__(64) rel_dkv_kernel(Args a, const T* __restrict__ qkv, const T* __restrict__ d_o, const float* __restrict__ stats,
+__global__ void __launch_bounds__(64) rel_dkv_kernel(RelArgs a, const T* __restrict__ qkv, const T* __restrict__ d_o, const float* __restrict__ stats,
                                                      const float* __restrict__ delta, T* __restrict__ dqkv) {
   __shared__ float f[64], e[64];
-  const int bh = blockIdx.y, b = bh / a.heads, h = bh - b * a.heads, u = blockIdx.x, lane = threadIdx.x, d = a.heads * a.dh, n = tokens(a, b);
+  const int bh = blockIdx.x / a.T, b = bh / a.heads, h = bh - b * a.heads, u = blockIdx.x - bh * a.T, lane = threadIdx.x, d = a.heads * a.dh, n = rel_tokens(a, b);
   const size_t ld = 3 * (size_t)d;
   const T *base = qkv + (size_t)b * a.T * ld + h * a.dh, *g = d_o + (size_t)b * a.T * d + h * a.dh, *k = base + (size_t)u * ld + d;
   float dk[2] = {0.f, 0.f}, dv[2] = {0.f, 0.f};
@@ -192,7 +175,7 @@ __global__ void __launch_bounds__(64) rel_dkv_kernel(Args a, const T* __restrict
 
 // dx of every pair summed over the images, in the order of the plan: [heads][NT][NT][64][16]
 template <typename T>
-__global__ void __launch_bounds__(256) rel_pairs_kernel(Args a, const T* __restrict__ qkv, const T* __restrict__ d_o, const float* __restrict__ stats,
+__global__ void __launch_bounds__(256) rel_pairs_kernel(RelArgs a, const T* __restrict__ qkv, const T* __restrict__ d_o, const float* __restrict__ stats,
                                                         const float* __restrict__ delta, float* __restrict__ pairs) {
   const int h = blockIdx.y, d = a.heads * a.dh;
   const size_t ld = 3 * (size_t)d, i = (size_t)blockIdx.x * 256 + threadIdx.x;
@@ -201,7 +184,7 @@ __global__ void __launch_bounds__(256) rel_pairs_kernel(Args a, const T* __restr
   if (a.dr.q) key = rel_key(a.rng, a.site);
   float sum = 0.f;
   for (int b = 0; b < a.B; ++b) {
-    const int n = tokens(a, b), bh = b * a.heads + h;
+    const int n = rel_tokens(a, b), bh = b * a.heads + h;
     if (t >= n || u >= n) continue;
     const T *base = qkv + (size_t)b * a.T * ld + h * a.dh, *k = base + (size_t)u * ld + d, *g = d_o + ((size_t)b * a.T + t) * d + h * a.dh;
     const size_t row = (size_t)bh * a.T + t;
@@ -211,13 +194,17 @@ __global__ void __launch_bounds__(256) rel_pairs_kernel(Args a, const T* __restr
   pairs[((size_t)h * a.NT * a.NT + block) * 1024 + rel_place(u & 31, t & 31)] = sum;
 }
 
-// a workgroup to a bucket and head: its pairs in the order of its list
-__global__ void __launch_bounds__(256) rel_buckets_kernel(Args a, const float* __restrict__ pairs, float* __restrict__ dtable) {
+// a workgroup to a bucket and head: its pairs in the order of its list, the splits' sums one after the other
+__global__ void __launch_bounds__(256) rel_buckets_kernel(RelArgs a, const float* __restrict__ pairs, int splits, float* __restrict__ dtable) {
   __shared__ float sm[4];
   const int k = blockIdx.x, h = blockIdx.y, s0 = a.start[k], s1 = a.start[k + 1];
-  const float* m = pairs + (size_t)h * a.NT * a.NT * 1024;
+  const size_t map = (size_t)a.NT * a.NT * 1024;
+  const float* m = pairs + h * map;
   float s = 0.f;
-  for (int i = s0 + threadIdx.x; i < s1; i += 256) s += m[a.list[i]];
+  for (int i = s0 + threadIdx.x; i < s1; i += 256) {
+    const int at = a.list[i];
+    for (int k = 0; k < splits; ++k) s += m[k * a.heads * map + at];
+  }
   s = wave_sum(s);
   if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = s;
   __syncthreads();
@@ -232,13 +219,14 @@ int check(const cnnk_rel_desc* d, RelDrop* dr) {
   if (d->dtype != CNNK_F32 && d->dtype != CNNK_BF16) return CNNK_ERR_UNSUPPORTED;
   if (d->dh != 16 && d->dh != 32 && d->dh != 64 && d->dh != 128) return CNNK_ERR_UNSUPPORTED;
   if (d->T > 2 * kRelMaxT || (d->buckets && (d->T > kRelMaxT || d->buckets > kRelMaxBuckets))) return CNNK_ERR_UNSUPPORTED;
-  if ((double)d->T * 3 * d->heads * d->dh * elem_size(d->dtype) >= 2147483648.0 || (double)d->B * d->heads > 65535.0) return CNNK_ERR_UNSUPPORTED;
+  if (d->heads > 65535 || (double)d->T * 3 * d->heads * d->dh * elem_size(d->dtype) >= 2147483648.0 || (double)d->B * d->heads * ((d->T + 31) / 32) > 2147483647.0 / 32) return CNNK_ERR_UNSUPPORTED;
   return CNNK_OK;
 }
-Args args_of(const cnnk_rel_desc* d, RelDrop dr, const float* table, const void* plan, const int* lens, const unsigned long long* rng) {
-  Args a;
+RelArgs args_of(const cnnk_rel_desc* d, RelDrop dr, const float* table, const void* plan, const int* lens, const unsigned long long* rng) {
+  RelArgs a;
   a.B = d->B;
   a.T = d->T;
+  a.Tp = (d->T + 63) / 64 * 64;
   a.heads = d->heads;
   a.dh = d->dh;
   a.NT = (d->T + 31) / 32;
@@ -247,65 +235,66 @@ Args args_of(const cnnk_rel_desc* d, RelDrop dr, const float* table, const void*
   a.site = d->site;
   a.dr = dr;
   a.table = table;
-  a.by_query = nullptr;
+  a.by_query = a.by_key = nullptr;
   a.start = a.list = nullptr;
   a.lens = lens;
   a.rng = rng;
   if (d->buckets) {
     const RelPlan at = rel_plan_layout(d->T, d->buckets);
     a.by_query = (const unsigned short*)((const char*)plan + at.by_query);
+    a.by_key = (const unsigned short*)((const char*)plan + at.by_key);
     a.start = (const int*)((const char*)plan + at.start);
     a.list = (const int*)((const char*)plan + at.list);
   }
   return a;
 }
-size_t delta_bytes(const cnnk_rel_desc* d) { return align_up((size_t)d->B * d->heads * d->T * 4, 256); }
+// scratch of the backward pass: three floats for each row, and the sums of every pair, `splits` times over
+size_t rows_bytes(const cnnk_rel_desc* d) { return align_up((size_t)d->B * d->heads * 3 * ((d->T + 63) / 64 * 64) * 4, 256); }
+int splits_of(const cnnk_rel_desc* d) {
+  if (d->dtype == CNNK_F32) return 1;
+  const long NT = (d->T + 31) / 32, groups = d->heads * ((NT + 1) / 2) * ((NT + 3) / 4), want = (512 + groups - 1) / groups;
+  return (int)(want < d->B ? want : d->B);
+}
 size_t pairs_bytes(const cnnk_rel_desc* d) {
   const size_t NT = (d->T + 31) / 32;
-  return (size_t)d->heads * NT * NT * 4096;
+  return (size_t)splits_of(d) * d->heads * NT * NT * 4096;
 }
 
-template <typename T>
-int fwd(const Args& a, const void* qkv, void* o, void* o_rest, float* stats, hipStream_t st) {
-  rel_fwd_kernel<T><<<dim3(a.T, a.B * a.heads), 64, 0, st>>>(a, (const T*)qkv, (T*)o, (T*)o_rest, stats);
+int fwd_f32(const RelArgs& a, const float* qkv, float* o, float* stats, hipStream_t st) {
+  rel_fwd_kernel<float><<<(unsigned)(a.T * a.B * a.heads), 64, 0, st>>>(a, qkv, o, stats);
   return launch_status();
 }
-template <typename T>
-int bwd(const Args& a, const void* qkv_, const void* o, const void* o_rest, const void* d_o_, const float* stats, void* dqkv, float* dtable, float* delta, float* pairs,
-        hipStream_t st) {
-  const T *qkv = (const T*)qkv_, *d_o = (const T*)d_o_;
-  const size_t rows = (size_t)a.B * a.heads * a.T;
-  rel_delta_kernel<T><<<(unsigned)((rows + 15) / 16), 256, 0, st>>>(a, (const T*)o, sizeof(T) == 2 ? (const T*)o_rest : nullptr, d_o, delta);
-  rel_dq_kernel<T><<<dim3(a.T, a.B * a.heads), 64, 0, st>>>(a, qkv, d_o, stats, delta, (T*)dqkv);
-  rel_dkv_kernel<T><<<dim3(a.T, a.B * a.heads), 64, 0, st>>>(a, qkv, d_o, stats, delta, (T*)dqkv);
-  if (a.buckets && dtable) {
-    rel_pairs_kernel<T><<<dim3(a.NT * a.NT * 4, a.heads), 256, 0, st>>>(a, qkv, d_o, stats, delta, pairs);
-    rel_buckets_kernel<<<dim3(a.buckets, a.heads), 256, 0, st>>>(a, pairs, dtable);
-  }
+int bwd_f32(const RelArgs& a, const float* qkv, const float* o, const float* d_o, const float* stats, float* dqkv, float* rows, float* pairs, hipStream_t st) {
+  const unsigned n = (unsigned)(a.T * a.B * a.heads);
+  rel_delta_kernel<float><<<(n + 15) / 16, 256, 0, st>>>(a, o, d_o, rows);
+  rel_dq_kernel<float><<<n, 64, 0, st>>>(a, qkv, d_o, stats, rows, dqkv);
+  rel_dkv_kernel<float><<<n, 64, 0, st>>>(a, qkv, d_o, stats, rows, dqkv);
+  if (pairs) rel_pairs_kernel<float><<<dim3(a.NT * a.NT * 4, a.heads), 256, 0, st>>>(a, qkv, d_o, stats, rows, pairs);
   return launch_status();
 }
 }  // namespace
 
 extern "C" int cnnk_rel_attention_fwd(const cnnk_rel_desc* d, const void* qkv, const float* table, const void* plan, const int* lens, const unsigned long long* rng,
-                                      void* o, void* o_rest, float* stats, void* stream) {
+                                      void* o, float* stats, void* stream) {
   RelDrop dr;
   const int rc = check(d, &dr);
   if (rc != CNNK_OK) return rc;
   if (!qkv || !o || (d->buckets && (!table || !plan)) || (dr.q && !rng)) return CNNK_ERR_NULL;
-  if (!rel_aligned(qkv, 16) || !rel_aligned(o, 16) || !rel_aligned(o_rest, 16) || !rel_aligned(stats, 8) || !rel_aligned(table, 4) || !rel_aligned(plan, 256) ||
+  if (!rel_aligned(qkv, 16) || !rel_aligned(o, 16) || !rel_aligned(stats, 8) || !rel_aligned(table, 4) || !rel_aligned(plan, 256) ||
       !rel_aligned(lens, 4) || !rel_aligned(rng, 8))
     return CNNK_ERR_UNSUPPORTED;
-  const Args a = args_of(d, dr, table, plan, lens, rng);
-  return d->dtype == CNNK_BF16 ? fwd<bf16_t>(a, qkv, o, o_rest, stats, (hipStream_t)stream) : fwd<float>(a, qkv, o, nullptr, stats, (hipStream_t)stream);
+  const RelArgs a = args_of(d, dr, table, plan, lens, rng);
+  hipStream_t st = (hipStream_t)stream;
+  return d->dtype == CNNK_BF16 ? rel_mfma_fwd(a, qkv, o, stats, st) : fwd_f32(a, (const float*)qkv, (float*)o, stats, st);
 }
 
 extern "C" size_t cnnk_rel_attention_workspace_bytes(const cnnk_rel_desc* d) {
   RelDrop dr;
   if (check(d, &dr) != CNNK_OK) return 0;
-  return delta_bytes(d) + (d->buckets ? pairs_bytes(d) : 0);
+  return rows_bytes(d) + (d->buckets ? pairs_bytes(d) : 0);
 }
 
-extern "C" int cnnk_rel_attention_bwd(const cnnk_rel_desc* d, const void* qkv, const void* o, const void* o_rest, const void* d_o, const float* table, const void* plan,
+extern "C" int cnnk_rel_attention_bwd(const cnnk_rel_desc* d, const void* qkv, const void* o, const void* d_o, const float* table, const void* plan,
                                       const int* lens, const unsigned long long* rng, const float* stats, void* dqkv, float* dtable, void* ws, size_t ws_bytes,
                                       void* stream) {
   RelDrop dr;
@@ -313,12 +302,16 @@ extern "C" int cnnk_rel_attention_bwd(const cnnk_rel_desc* d, const void* qkv, c
   if (rc != CNNK_OK) return rc;
   if (!qkv || !o || !d_o || !stats || !dqkv || (d->buckets && (!table || !plan)) || (dr.q && !rng)) return CNNK_ERR_NULL;
   if (!ws || ws_bytes < cnnk_rel_attention_workspace_bytes(d)) return CNNK_ERR_WORKSPACE;
-  if (!rel_aligned(qkv, 16) || !rel_aligned(o, 16) || !rel_aligned(o_rest, 16) || !rel_aligned(d_o, 16) || !rel_aligned(stats, 8) || !rel_aligned(table, 4) ||
+  if (!rel_aligned(qkv, 16) || !rel_aligned(o, 16) || !rel_aligned(d_o, 16) || !rel_aligned(stats, 8) || !rel_aligned(table, 4) ||
       !rel_aligned(plan, 256) || !rel_aligned(lens, 4) || !rel_aligned(rng, 8) || !rel_aligned(dqkv, 16) || !rel_aligned(dtable, 4) || !rel_aligned(ws, 256))
     return CNNK_ERR_UNSUPPORTED;
-  const Args a = args_of(d, dr, table, plan, lens, rng);
-  float *delta = (float*)ws, *pairs = (float*)((char*)ws + delta_bytes(d));
+  const RelArgs a = args_of(d, dr, table, plan, lens, rng);
+  float *rows = (float*)ws, *pairs = d->buckets && dtable ? (float*)((char*)ws + rows_bytes(d)) : nullptr;
   hipStream_t st = (hipStream_t)stream;
-  return d->dtype == CNNK_BF16 ? bwd<bf16_t>(a, qkv, o, o_rest, d_o, stats, dqkv, dtable, delta, pairs, st)
-                               : bwd<float>(a, qkv, o, nullptr, d_o, stats, dqkv, dtable, delta, pairs, st);
+  const int splits = splits_of(d);
+  const int r = d->dtype == CNNK_BF16 ? rel_mfma_bwd(a, qkv, o, d_o, stats, dqkv, rows, pairs, splits, st)
+                                      : bwd_f32(a, (const float*)qkv, (const float*)o, (const float*)d_o, stats, (float*)dqkv, rows, pairs, st);
+  if (r != CNNK_OK || !pairs) return r;
+  rel_buckets_kernel<<<dim3(d->buckets, d->heads), 256, 0, st>>>(a, pairs, splits, dtable);
+  return launch_status();
 }

@@ -34,10 +34,10 @@ def _declare():
     lib.cnnk_rel_plan_bytes.restype = lib.cnnk_rel_plan_workspace_bytes.restype = sz
     lib.cnnk_rel_plan_bytes.argtypes = lib.cnnk_rel_plan_workspace_bytes.argtypes = [ci, ci]
     lib.cnnk_rel_plan.argtypes = [ci, ci, vp, vp, vp, sz, vp]
-    lib.cnnk_rel_attention_fwd.argtypes = [rd] + [vp] * 9
+    lib.cnnk_rel_attention_fwd.argtypes = [rd] + [vp] * 8
     lib.cnnk_rel_attention_workspace_bytes.restype = sz
     lib.cnnk_rel_attention_workspace_bytes.argtypes = [rd]
-    lib.cnnk_rel_attention_bwd.argtypes = [rd] + [vp] * 12 + [sz, vp]
+    lib.cnnk_rel_attention_bwd.argtypes = [rd] + [vp] * 11 + [sz, vp]
 
 
 _declare()
@@ -103,16 +103,15 @@ def rel_desc(B, T, heads, dh, dtype, buckets=0, p=0.0, site=0):
     return RelDesc(B, T, heads, dh, dtype, buckets, p, site)
 
 
-def cnnk_rel_attention_fwd(d, qkv, table, plan, lens, rng, o, o_rest=None, stats=None, stream=0):
-    _check(lib.cnnk_rel_attention_fwd(C.byref(d), ptr(qkv), ptr(table), ptr(plan), ptr(lens), ptr(rng), ptr(o), ptr(o_rest),
-                                      ptr(stats), stream), "cnnk_rel_attention_fwd")
+def cnnk_rel_attention_fwd(d, qkv, table, plan, lens, rng, o, stats=None, stream=0):
+    _check(lib.cnnk_rel_attention_fwd(C.byref(d), ptr(qkv), ptr(table), ptr(plan), ptr(lens), ptr(rng), ptr(o), ptr(stats), stream), "cnnk_rel_attention_fwd")
 
 
 def cnnk_rel_attention_workspace_bytes(d):
     return int(lib.cnnk_rel_attention_workspace_bytes(C.byref(d)))
 
 
-def cnnk_rel_attention_bwd(d, qkv, o, o_rest, d_o, table, plan, lens, rng, stats, dqkv, dtable, ws, ws_bytes, stream=0):
-    _check(lib.cnnk_rel_attention_bwd(C.byref(d), ptr(qkv), ptr(o), ptr(o_rest), ptr(d_o), ptr(table), ptr(plan), ptr(lens),
+def cnnk_rel_attention_bwd(d, qkv, o, d_o, table, plan, lens, rng, stats, dqkv, dtable, ws, ws_bytes, stream=0):
+    _check(lib.cnnk_rel_attention_bwd(C.byref(d), ptr(qkv), ptr(o), ptr(d_o), ptr(table), ptr(plan), ptr(lens),
                                       ptr(rng), ptr(stats), ptr(dqkv), ptr(dtable), ptr(ws), ws_bytes, stream),
            "cnnk_rel_attention_bwd")

@@ -83,9 +83,9 @@ def test_maps_and_plans_refuse_bad_arguments():
 def test_attention_refuses_bad_arguments():
     ok = rel.rel_desc(2, 17, 2, 64, cnnk.BF16, 52, 0.1)
     big = 1 << 40
-    fwd = lambda d, qkv=A, table=A, plan=A, lens=A, rng=A, o=A, rest=A, stats=A: rel.cnnk_rel_attention_fwd(d, qkv, table, plan, lens, rng, o, rest, stats)
-    bwd = lambda d, qkv=A, o=A, rest=A, d_o=A, table=A, plan=A, lens=A, rng=A, stats=A, dqkv=A, dtable=A, ws=A, n=big: \
-        rel.cnnk_rel_attention_bwd(d, qkv, o, rest, d_o, table, plan, lens, rng, stats, dqkv, dtable, ws, n)
+    fwd = lambda d, qkv=A, table=A, plan=A, lens=A, rng=A, o=A, stats=A: rel.cnnk_rel_attention_fwd(d, qkv, table, plan, lens, rng, o, stats)
+    bwd = lambda d, qkv=A, o=A, d_o=A, table=A, plan=A, lens=A, rng=A, stats=A, dqkv=A, dtable=A, ws=A, n=big: \
+        rel.cnnk_rel_attention_bwd(d, qkv, o, d_o, table, plan, lens, rng, stats, dqkv, dtable, ws, n)
     D = lambda B=2, T=17, heads=2, dh=64, dt=cnnk.BF16, n=52, p=0.1: rel.rel_desc(B, T, heads, dh, dt, n, p)
     for d, status in ((D(B=0), SHAPE), (D(T=0), SHAPE), (D(heads=0), SHAPE), (D(dh=0), SHAPE), (D(n=-1), SHAPE), (D(p=1.0), SHAPE), (D(p=-0.5), SHAPE),
                       (D(p=float("nan")), SHAPE), (D(dh=48), UNSUPPORTED), (D(dh=256), UNSUPPORTED), (D(dt=5), UNSUPPORTED), (D(T=8193), UNSUPPORTED),
@@ -96,12 +96,12 @@ def test_attention_refuses_bad_arguments():
     for k in ("qkv", "table", "plan", "rng", "o"):
         refused(NULL, fwd, ok, **{k: None})
         refused(UNSUPPORTED, fwd, ok, **{k: A + 2})
-    for k in ("lens", "rest", "stats"):
+    for k in ("lens", "stats"):
         refused(UNSUPPORTED, fwd, ok, **{k: A + 2})
     for k in ("qkv", "o", "d_o", "table", "plan", "rng", "stats", "dqkv"):
         refused(NULL, bwd, ok, **{k: None})
         refused(UNSUPPORTED, bwd, ok, **{k: A + 2})
-    for k in ("lens", "rest", "dtable", "ws"):
+    for k in ("lens", "dtable", "ws"):
         refused(UNSUPPORTED, bwd, ok, **{k: A + 2})
     need = rel.cnnk_rel_attention_workspace_bytes(ok)
     assert need > rel.cnnk_rel_attention_workspace_bytes(D(n=0)) > 0
