@@ -48,7 +48,7 @@ static inline bool rel_aligned(const void* p, size_t a) { return ((size_t)p & (a
 //   by_key    a lane a key, its registers queries, block (u / 32, t / 32)
 // An entry is 4 x bucket, the byte offset into a head's table in LDS; 4 x buckets for masked pairs and for padding, where that table holds -infinity.
 //   start     int [buckets + 1]: where a bucket's pairs begin in
-//   list      int [T * T]: places of its pairs in by_query, in the order of (t, u)
+//   list      int [T * T]: places of its pairs in a head's sums of dx (rel_sum_place), in the order of (t, u)
 constexpr int kRelMaxT = 8192, kRelMaxBuckets = 16382;
 struct RelPlan { size_t by_query, by_key, start, list, bytes; };
 static inline RelPlan rel_plan_layout(int T, int buckets) {
@@ -63,3 +63,9 @@ static inline RelPlan rel_plan_layout(int T, int buckets) {
 }
 // place of row r, column c of a block in its 1024 entries
 __host__ __device__ __forceinline__ int rel_place(int r, int c) { return (((r >> 2 & 1) << 5 | c) << 4) | (r >> 3) << 2 | (r & 3); }
+// place of a pair in the sums of dx over images: blocks as in by_key, in a block registers in fours [4][64 lanes][4], which a wavefront loads and
+// stores 1 KB at a time
+__host__ __device__ __forceinline__ int rel_sum_place(int NT, int t, int u) {
+  const int r = t & 31;
+  return ((u >> 5) * NT + (t >> 5)) * 1024 + (r >> 3) * 256 + ((r >> 2 & 1) << 5 | (u & 31)) * 4 + (r & 3);
+}

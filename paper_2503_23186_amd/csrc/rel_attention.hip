@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(64) rel_dkv_kernel(RelArgs a, const T* __restr
     }
 }
 
-// dx of every pair summed over the images, in the order of the plan: [heads][NT][NT][64][16]
+// dx of every pair summed over the images, in the order of the plan's list: [heads][NT][NT][4][64][4]
 template <typename T>
 __global__ void __launch_bounds__(256) rel_pairs_kernel(RelArgs a, const T* __restrict__ qkv, const T* __restrict__ d_o, const float* __restrict__ stats,
                                                         const float* __restrict__ delta, float* __restrict__ pairs) {
@@ -191,24 +191,48 @@ __global__ void __launch_bounds__(256) rel_pairs_kernel(RelArgs a, const T* __re
     const float p = prob(score(a, dot_rows(base + (size_t)t * ld, k, a.dh), t, u, h), stats + row * 2);
     sum += p * (keep(a, key, bh, t, u) * dot_rows(g, k + d, a.dh) - delta[row]);
   }
-  pairs[((size_t)h * a.NT * a.NT + block) * 1024 + rel_place(u & 31, t & 31)] = sum;
+  pairs[(size_t)h * a.NT * a.NT * 1024 + rel_sum_place(a.NT, t, u)] = sum;
 }
 
-// a workgroup to a bucket and head: its pairs in the order of its list, the splits' sums one after the other
-__global__ void __launch_bounds__(256) rel_buckets_kernel(RelArgs a, const float* __restrict__ pairs, int splits, float* __restrict__ dtable) {
-  __shared__ float sm[4];
-  const int k = blockIdx.x, h = blockIdx.y, s0 = a.start[k], s1 = a.start[k + 1];
-  const size_t map = (size_t)a.NT * a.NT * 1024;
-  const float* m = pairs + h * map;
-  float s = 0.f;
-  for (int i = s0 + threadIdx.x; i < s1; i += 256) {
-    const int at = a.list[i];
-    for (int k = 0; k < splits; ++k) s += m[k * a.heads * map + at];
+// the splits' sums of the pairs into the first's place
+__global__ void __launch_bounds__(256) rel_splits_kernel(float4* pairs, size_t n, int splits) {
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  float4 s = pairs[i];
+  for (int k = 1; k < splits; ++k) {
+    const float4 v = pairs[k * n + i];
+    s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
   }
-  s = wave_sum(s);
-  if ((threadIdx.x & 63) == 0) sm[threadIdx.x >> 6] = s;
-  __syncthreads();
-  if (threadIdx.x == 0) dtable[(size_t)k * a.heads + h] = (sm[0] + sm[1]) + (sm[2] + sm[3]);
+  pairs[i] = s;
+}
+
+// `lanes` threads to a bucket and head, which take its pairs by turns; a workgroup has neighbouring buckets, whose pairs lie beside each other
+// in maps by distance.
+__global__ void __launch_bounds__(256) rel_buckets_kernel(RelArgs a, const float* __restrict__ pairs, int lanes, float* __restrict__ dtable) {
+  __shared__ float sm[256];
+  const int per = 256 / lanes, k = blockIdx.x * per + threadIdx.x / lanes, h = blockIdx.y, j = threadIdx.x & (lanes - 1);
+  const float* m = pairs + (size_t)h * a.NT * a.NT * 1024;
+  float s = 0.f;
+  if (k < a.buckets) {
+    const int s1 = a.start[k + 1];
+    int i = a.start[k] + j;
+    for (; i + 3 * lanes < s1; i += 4 * lanes) {
+      int at[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) at[e] = a.list[i + e * lanes];
+      float v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = m[at[e]];
+      s += (v[0] + v[1]) + (v[2] + v[3]);
+    }
+    for (; i < s1; i += lanes) s += m[a.list[i]];
+  }
+  sm[threadIdx.x] = s;
+  for (int w = lanes >> 1; w > 0; w >>= 1) {
+    __syncthreads();
+    if (j < w) sm[threadIdx.x] += sm[threadIdx.x + w];
+  }
+  if (j == 0 && k < a.buckets) dtable[(size_t)k * a.heads + h] = sm[threadIdx.x];
 }
 
 int check(const cnnk_rel_desc* d, RelDrop* dr) {
@@ -252,7 +276,7 @@ RelArgs args_of(const cnnk_rel_desc* d, RelDrop dr, const float* table, const vo
 size_t rows_bytes(const cnnk_rel_desc* d) { return align_up((size_t)d->B * d->heads * 3 * ((d->T + 63) / 64 * 64) * 4, 256); }
 int splits_of(const cnnk_rel_desc* d) {
   if (d->dtype == CNNK_F32) return 1;
-  const long NT = (d->T + 31) / 32, groups = d->heads * ((NT + 1) / 2) * ((NT + 3) / 4), want = (512 + groups - 1) / groups;
+  const long NT = (d->T + 31) / 32, groups = d->heads * ((NT + 3) / 4), want = (512 + groups - 1) / groups;
   return (int)(want < d->B ? want : d->B);
 }
 size_t pairs_bytes(const cnnk_rel_desc* d) {
@@ -312,6 +336,13 @@ extern "C" int cnnk_rel_attention_bwd(const cnnk_rel_desc* d, const void* qkv, c
   const int r = d->dtype == CNNK_BF16 ? rel_mfma_bwd(a, qkv, o, d_o, stats, dqkv, rows, pairs, splits, st)
                                       : bwd_f32(a, (const float*)qkv, (const float*)o, (const float*)d_o, stats, (float*)dqkv, rows, pairs, st);
   if (r != CNNK_OK || !pairs) return r;
-  rel_buckets_kernel<<<dim3(d->buckets, d->heads), 256, 0, st>>>(a, pairs, splits, dtable);
+  if (splits > 1) {
+    const size_t n = (size_t)d->heads * a.NT * a.NT * 256;
+    rel_splits_kernel<<<(unsigned)((n + 255) / 256), 256, 0, st>>>((float4*)pairs, n, splits);
+  }
+  // enough threads to fill the device where buckets are few
+  int lanes = 8;
+  while (lanes < 256 && (long)d->buckets * d->heads * lanes < 131072) lanes *= 2;
+  rel_buckets_kernel<<<dim3((d->buckets + 256 / lanes - 1) / (256 / lanes), d->heads), 256, 0, st>>>(a, pairs, lanes, dtable);
   return launch_status();
 }

@@ -8,8 +8,9 @@
 //
 // The bias: the plan (rel.h) holds the bucket map in the order of the accumulator's registers, 32 bytes a lane and tile, as byte offsets into the head's
 // column of the table, which lies in LDS; the entry behind its end is -infinity, which masked pairs and tokens past T name.
-// Scores are formed as q.k / sqrt(dh) + bias and the reference is subtracted from the sum, so that tables with the lowest finite
-// value keep their meaning; the exponential's base rides in the multiply-add in front of it.
+// Where 1 / sqrt(dh) is a power of two it goes into q (exact in bf16) and the bias into the accumulator that a score tile starts from; otherwise both
+// meet in a multiply-add.  The reference is subtracted from the sum, so that tables with the lowest finite value keep their meaning; the
+// exponential's base rides in the multiply-add behind it.
 //
 // dx = P (dP - delta) with delta = sum P dP.  do . o is delta up to what rounding took off o and off the probabilities in front of it, 2^-7 of its
 // terms, which would show in the table's gradient (an fp32 sum).  The walk for dq therefore takes it as an estimate: dx' = P (dP - estimate) sums to what the
@@ -32,6 +33,7 @@ constexpr float kSlack = 5.5f, kDown = 22.f;
 template <int DH> struct Dim {
   static constexpr int NK = DH / 16, NM = (DH + 31) / 32;
   static constexpr int PLANE = KB * ROW_B, MAT = NM * PLANE, STAGE = 2 * MAT;
+  static constexpr bool EXACT = DH == 16 || DH == 64;      // 1 / sqrt(DH) is a power of two
 };
 
 // ---- stages: rows r0 .. r0 + 63 of two matrices ------------------------------------------------------------------------
@@ -61,18 +63,14 @@ template <int DH> struct Stager {
 };
 
 // ---- bias ------------------------------------------------------------------------------------------------------------------
-struct MapRegs { uint4 v[4]; };      // two tiles
-__device__ __forceinline__ void map_load(MapRegs& m, const unsigned short* map, int tile, int last, int lane) {
+struct MapRegs { uint4 v[2]; };
+__device__ __forceinline__ void map_load(MapRegs& m, const unsigned short* map, int tile, int lane) {
   const uint4* p = reinterpret_cast<const uint4*>(map + (size_t)tile * 1024 + lane * 16);
   m.v[0] = p[0];
   m.v[1] = p[1];
-  if (tile < last) {
-    m.v[2] = p[128];
-    m.v[3] = p[129];
-  }
 }
-__device__ __forceinline__ float bias_of(const unsigned char* table, const uint4* v, int i) {
-  const uint4 q = v[i >> 3];
+__device__ __forceinline__ float bias_of(const unsigned char* table, const MapRegs& m, int i) {
+  const uint4 q = m.v[i >> 3];
   const unsigned w = (i & 7) < 4 ? ((i & 7) < 2 ? q.x : q.y) : ((i & 7) < 6 ? q.z : q.w);
   return *reinterpret_cast<const float*>(table + (i & 1 ? w >> 16 : w & 0xffffu));
 }
@@ -80,6 +78,39 @@ __device__ __forceinline__ float bias_of(const unsigned char* table, const uint4
 __device__ __forceinline__ void table_put(float* dst, const RelArgs& a, int h) {
   for (int k = threadIdx.x; k < a.buckets; k += blockDim.x) dst[k] = a.table[(size_t)k * a.heads + h];
   if (threadIdx.x == 0) dst[a.buckets] = -INFINITY;
+}
+
+// q times 1 / sqrt(DH) where that is exact
+template <int DH> __device__ __forceinline__ void scale_frags(bf16x8_t* f) {
+  if (!Dim<DH>::EXACT) return;
+#pragma unroll
+  for (int k = 0; k < Dim<DH>::NK; ++k) {
+    float v[8];
+    unpack8(__builtin_bit_cast(uint4, f[k]), v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= DH == 64 ? 0.125f : 0.25f;
+    f[k] = __builtin_bit_cast(bf16x8_t, uint4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])});
+  }
+}
+// A tile of scores with their bias.  One operand has been through scale_frags.
+template <int DH, bool BIAS>
+__device__ __forceinline__ f32x16_t score_tile(const unsigned char* a, const bf16x8_t* b, const float* table, const MapRegs& m, float scale, int lane) {
+  const unsigned char* t = reinterpret_cast<const unsigned char*>(table);
+  f32x16_t x;
+  if (BIAS && Dim<DH>::EXACT) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = bias_of(t, m, i);
+  } else {
+    x = zero16();
+  }
+#pragma unroll
+  for (int k = 0; k < Dim<DH>::NK; ++k)
+    x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_read(a, Dim<DH>::PLANE, lane & 31, k * 16 + (lane >> 5) * 8), b[k], x, 0, 0, 0);
+  if (!Dim<DH>::EXACT) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = BIAS ? fmaf(x[i], scale, bias_of(t, m, i)) : x[i] * scale;
+  }
+  return x;
 }
 
 // ---- dropout ---------------------------------------------------------------------------------------------------------------
@@ -141,8 +172,8 @@ __device__ __forceinline__ int key_of(int i, int h) { return (i >> 2) * 8 + h * 
 
 // ---- forward ---------------------------------------------------------------------------------------------------------------
 template <int DH, bool BIAS, bool DROP>
-__global__ void __launch_bounds__(256) rel_mfma_fwd_kernel(RelArgs a, const bf16_t* __restrict__ qkv, bf16_t* __restrict__ o,
-                                                           float* __restrict__ stats, int parts) {
+__global__ void __launch_bounds__(256, DH <= 64 ? 3 : 2) rel_mfma_fwd_kernel(RelArgs a, const bf16_t* __restrict__ qkv, bf16_t* __restrict__ o,
+                                                                             float* __restrict__ stats, int parts) {
   using D = Dim<DH>;
   extern __shared__ __align__(16) unsigned char smem[];
   int bh, part;
@@ -161,81 +192,75 @@ __global__ void __launch_bounds__(256) rel_mfma_fwd_kernel(RelArgs a, const bf16
     Stager<DH> st;
     st.init(base + d, base + 2 * d, (unsigned)ld * 2, (unsigned)ld * 2, n, lane);
     st.load(0, 0, wave, waves);
-    const unsigned short* map = nullptr;
-    MapRegs mr, next;
     const bool mine = q0 < n;
+    const unsigned short* map = BIAS ? a.by_query + (size_t)(q0 >> 5) * a.NT * 1024 : nullptr;
+    MapRegs mr, next;
     if (BIAS) {
-      if (mine) {
-        map = a.by_query + (size_t)(q0 >> 5) * a.NT * 1024;
-        map_load(next, map, 0, a.NT - 1, lane);
-      }
+      if (mine) map_load(next, map, 0, lane);
       table_put(table, a, head);
     }
     bf16x8_t bq[D::NK];
     own_frags<D::NK>(base, ld, q, n, h, bq);
+    scale_frags<DH>(bq);
     RelKey key{0u, 0u};
     if (DROP) key = rel_key(a.rng, a.site);
-    const int stages = (n + KB - 1) / KB;
-    for (int s = 0; s < stages; ++s) {
-      wait_vm<0>();
-      workgroup_barrier();
-      mr = next;
-      if (s + 1 < stages) {
-        st.load((s + 1) * KB, ((s + 1) & 1) * D::STAGE, wave, waves);
-        if (BIAS && mine) map_load(next, map, 2 * (s + 1), a.NT - 1, lane);
+    const int tiles = (n + 31) >> 5;
+    for (int t = 0; t < tiles; ++t) {
+      if ((t & 1) == 0) {
+        wait_vm<0>();
+        workgroup_barrier();
+        if (t + 2 < tiles) st.load(t * 32 + KB, ((t >> 1) + 1 & 1) * D::STAGE, wave, waves);
       }
-      const unsigned char *Ks = smem + (s & 1) * D::STAGE, *Vs = Ks + D::MAT;
+      if (!mine) continue;
+      if (BIAS) {
+        mr = next;
+        if (t + 1 < tiles) map_load(next, map, t + 1, lane);
+      }
+      const unsigned char *Ks = smem + (t >> 1 & 1) * D::STAGE + (t & 1) * 32 * ROW_B, *Vs = Ks + D::MAT;
+      f32x16_t x = score_tile<DH, BIAS>(Ks, bq, table, mr, a.scale, lane);
+      if (t * 32 + 32 > n) {
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int k0 = s * KB + half * 32;
-        if (!mine || k0 >= n) break;
-        f32x16_t x = tile_nt<D::NK>(Ks, D::PLANE, half * 32, bq, lane);
+        for (int i = 0; i < 16; ++i)
+          if (t * 32 + key_of(i, h) >= n) x[i] = -INFINITY;
+      }
+      float tm = x[0];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = BIAS ? fmaf(x[i], a.scale, bias_of(reinterpret_cast<const unsigned char*>(table), mr.v + 2 * half, i)) : x[i] * a.scale;
-        if (k0 + 32 > n) {
+      for (int i = 1; i < 16; ++i) tm = fmaxf(tm, x[i]);
+      tm = both_halves_max(tm);
+      if (__any(tm > m + kSlack)) {
+        const float mn = fmaxf(m, tm);
+        const float f = m == mn ? 1.f : __builtin_amdgcn_exp2f((m - mn) * kLog2e);      // also where both are -infinity
+        l *= f;
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (k0 + key_of(i, h) >= n) x[i] = -INFINITY;
+        for (int mt = 0; mt < D::NM; ++mt)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) oacc[mt][i] *= f;
+        m = mn;
+      }
+      const float ref = m > -INFINITY ? m : 0.f;
+      float add[2] = {0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        x[i] = __builtin_amdgcn_exp2f(fmaf(x[i] - ref, kLog2e, -kDown));
+        add[i & 1] += x[i];
+      }
+      l += add[0] + add[1];
+      if (DROP) {
+        unsigned word[8];
+        draws_by_query(word, t * 32, (unsigned)q >> 2, (unsigned)bh, key, lane);
+        const unsigned q16 = a.dr.q << 16;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          x[2 * j] = word[j] << 16 < q16 ? 0.f : x[2 * j];
+          x[2 * j + 1] = word[j] < q16 ? 0.f : x[2 * j + 1];
         }
-        float tm = x[0];
+      }
 #pragma unroll
-        for (int i = 1; i < 16; ++i) tm = fmaxf(tm, x[i]);
-        tm = both_halves_max(tm);
-        if (__any(tm > m + kSlack)) {
-          const float mn = fmaxf(m, tm);
-          const float f = m == mn ? 1.f : __builtin_amdgcn_exp2f((m - mn) * kLog2e);      // also where both are -infinity
-          l *= f;
+      for (int j = 0; j < 2; ++j) {
+        const bf16x8_t pb = pack_frag(x, j);
 #pragma unroll
-          for (int mt = 0; mt < D::NM; ++mt)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) oacc[mt][i] *= f;
-          m = mn;
-        }
-        const float ref = m > -INFINITY ? m : 0.f;
-        float add[2] = {0.f, 0.f};
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          x[i] = __builtin_amdgcn_exp2f(fmaf(x[i] - ref, kLog2e, -kDown));
-          add[i & 1] += x[i];
-        }
-        l += add[0] + add[1];
-        if (DROP) {
-          unsigned word[8];
-          draws_by_query(word, k0, (unsigned)q >> 2, (unsigned)bh, key, lane);
-          const unsigned q16 = a.dr.q << 16;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            x[2 * j] = word[j] << 16 < q16 ? 0.f : x[2 * j];
-            x[2 * j + 1] = word[j] < q16 ? 0.f : x[2 * j + 1];
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const bf16x8_t pb = pack_frag(x, j);
-#pragma unroll
-          for (int mt = 0; mt < D::NM; ++mt)
-            oacc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_read_tr(Vs, D::PLANE, mt, half * 32 + 16 * j, lane), pb, oacc[mt], 0, 0, 0);
-        }
+        for (int mt = 0; mt < D::NM; ++mt)
+          oacc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_read_tr(Vs, D::PLANE, mt, 16 * j, lane), pb, oacc[mt], 0, 0, 0);
       }
     }
   }
@@ -247,19 +272,18 @@ __global__ void __launch_bounds__(256) rel_mfma_fwd_kernel(RelArgs a, const bf16
   for (int mt = 0; mt < D::NM; ++mt)
 #pragma unroll
     for (int i = 0; i < 16; ++i) oacc[mt][i] = any ? oacc[mt][i] * inv : 0.f;
-  const size_t at = ((size_t)b * a.T + q) * d + head * DH;
-  store_cols<DH>(o + at, oacc, h, q < a.T);
+  store_cols<DH>(o + ((size_t)b * a.T + q) * d + head * DH, oacc, h, q < a.T);
   if (stats && h == 0 && q < a.T)
     *reinterpret_cast<float2*>(stats + ((size_t)bh * a.T + q) * 2) = any ? float2{m, kLn2 * (__builtin_amdgcn_logf(l) + kDown)} : float2{-INFINITY, 0.f};
 }
 
-// ---- backward: dq, and for the kernels behind it the rows' statistics and delta ----------------------------------------------
+// ---- backward: dq, and for the kernel behind it the rows' statistics and delta -----------------------------------------------
 // rows [B * heads][3][Tp], Tp = T rounded up to 64: reference, log2 of the sum relative to it (+infinity for rows without a part: their probabilities
 // come out as 0), delta.
 template <int DH, bool BIAS, bool DROP>
-__global__ void __launch_bounds__(256) rel_mfma_dq_kernel(RelArgs a, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ o,
-                                                          const bf16_t* __restrict__ d_o, const float* __restrict__ stats, bf16_t* __restrict__ dqkv,
-                                                          float* __restrict__ rows, int parts) {
+__global__ void __launch_bounds__(256, DH <= 64 ? 2 : 1) rel_mfma_dq_kernel(RelArgs a, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ o,
+                                                                            const bf16_t* __restrict__ d_o, const float* __restrict__ stats,
+                                                                            bf16_t* __restrict__ dqkv, float* __restrict__ rows, int parts) {
   using D = Dim<DH>;
   extern __shared__ __align__(16) unsigned char smem[];
   int bh, part;
@@ -279,18 +303,16 @@ __global__ void __launch_bounds__(256) rel_mfma_dq_kernel(RelArgs a, const bf16_
     Stager<DH> st;
     st.init(base + d, base + 2 * d, (unsigned)ld * 2, (unsigned)ld * 2, n, lane);
     st.load(0, 0, wave, waves);
-    const unsigned short* map = nullptr;
-    MapRegs mr, next;
     const bool mine = q0 < n;
+    const unsigned short* map = BIAS ? a.by_query + (size_t)(q0 >> 5) * a.NT * 1024 : nullptr;
+    MapRegs mr, next;
     if (BIAS) {
-      if (mine) {
-        map = a.by_query + (size_t)(q0 >> 5) * a.NT * 1024;
-        map_load(next, map, 0, a.NT - 1, lane);
-      }
+      if (mine) map_load(next, map, 0, lane);
       table_put(table, a, head);
     }
     bf16x8_t bq[D::NK], bg[D::NK];
     own_frags<D::NK>(base, ld, q, n, h, bq);
+    scale_frags<DH>(bq);
     own_frags<D::NK>(d_o + head0, d, q, n, h, bg);
     {
       bf16x8_t t[D::NK];
@@ -308,51 +330,48 @@ __global__ void __launch_bounds__(256) rel_mfma_dq_kernel(RelArgs a, const bf16_
     }
     RelKey key{0u, 0u};
     if (DROP) key = rel_key(a.rng, a.site);
-    const int stages = (n + KB - 1) / KB;
-    for (int s = 0; s < stages; ++s) {
-      wait_vm<0>();
-      workgroup_barrier();
-      mr = next;
-      if (s + 1 < stages) {
-        st.load((s + 1) * KB, ((s + 1) & 1) * D::STAGE, wave, waves);
-        if (BIAS && mine) map_load(next, map, 2 * (s + 1), a.NT - 1, lane);
+    const int tiles = (n + 31) >> 5;
+    for (int t = 0; t < tiles; ++t) {
+      if ((t & 1) == 0) {
+        wait_vm<0>();
+        workgroup_barrier();
+        if (t + 2 < tiles) st.load(t * 32 + KB, ((t >> 1) + 1 & 1) * D::STAGE, wave, waves);
       }
-      const unsigned char *Ks = smem + (s & 1) * D::STAGE, *Vs = Ks + D::MAT;
+      if (!mine) continue;
+      if (BIAS) {
+        mr = next;
+        if (t + 1 < tiles) map_load(next, map, t + 1, lane);
+      }
+      const unsigned char *Ks = smem + (t >> 1 & 1) * D::STAGE + (t & 1) * 32 * ROW_B, *Vs = Ks + D::MAT;
+      f32x16_t p = score_tile<DH, BIAS>(Ks, bq, table, mr, a.scale, lane);
+      f32x16_t dx = tile_nt<D::NK>(Vs, D::PLANE, 0, bg, lane);
+      unsigned word[8];
+      if (DROP) draws_by_query(word, t * 32, (unsigned)q >> 2, (unsigned)bh, key, lane);
+      const unsigned q16 = a.dr.q << 16;
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int k0 = s * KB + half * 32;
-        if (!mine || k0 >= n) break;
-        f32x16_t p = tile_nt<D::NK>(Ks, D::PLANE, half * 32, bq, lane);
-        f32x16_t dx = tile_nt<D::NK>(Vs, D::PLANE, half * 32, bg, lane);
-        unsigned word[8];
-        if (DROP) draws_by_query(word, k0, (unsigned)q >> 2, (unsigned)bh, key, lane);
-        const unsigned q16 = a.dr.q << 16;
+      for (int i = 0; i < 16; ++i) {
+        p[i] = __builtin_amdgcn_exp2f(fmaf(p[i] - m, kLog2e, -L2));
+        float w = 1.f;
+        if (DROP) w = (i & 1 ? word[i >> 1] : word[i >> 1] << 16) < q16 ? 0.f : a.dr.scale;
+        dx[i] = p[i] * (DROP ? fmaf(dx[i], w, -delta) : dx[i] - delta);
+      }
+      if (t * 32 + 32 > n) {       // keys past the image's tokens: rows of zeros, whose probabilities may be infinite
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const float xi = BIAS ? fmaf(p[i], a.scale, bias_of(reinterpret_cast<const unsigned char*>(table), mr.v + 2 * half, i)) : p[i] * a.scale;
-          p[i] = __builtin_amdgcn_exp2f(fmaf(xi - m, kLog2e, -L2));
-          float w = 1.f;
-          if (DROP) w = (i & 1 ? word[i >> 1] : word[i >> 1] << 16) < q16 ? 0.f : a.dr.scale;
-          dx[i] = p[i] * (DROP ? fmaf(dx[i], w, -delta) : dx[i] - delta);
-        }
-        if (k0 + 32 > n) {       // keys past the image's tokens: rows of zeros, whose probabilities may be infinite
+        for (int i = 0; i < 16; ++i)
+          if (t * 32 + key_of(i, h) >= n) p[i] = dx[i] = 0.f;
+      }
+      float add[2] = {0.f, 0.f};
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (k0 + key_of(i, h) >= n) p[i] = dx[i] = 0.f;
-        }
-        float add[2] = {0.f, 0.f};
+      for (int i = 0; i < 16; ++i) add[i & 1] += dx[i];
+      lack += add[0] + add[1];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) add[i & 1] += dx[i];
-        lack += add[0] + add[1];
+      for (int j = 0; j < 2; ++j) {
+        const bf16x8_t pb = pack_frag(p, j), db = pack_frag(dx, j);
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const bf16x8_t pb = pack_frag(p, j), db = pack_frag(dx, j);
-#pragma unroll
-          for (int mt = 0; mt < D::NM; ++mt) {
-            const bf16x8_t k = frag_read_tr(Ks, D::PLANE, mt, half * 32 + 16 * j, lane);
-            dq[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, db, dq[mt], 0, 0, 0);
-            pk[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, pb, pk[mt], 0, 0, 0);
-          }
+        for (int mt = 0; mt < D::NM; ++mt) {
+          const bf16x8_t k = frag_read_tr(Ks, D::PLANE, mt, 16 * j, lane);
+          dq[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, db, dq[mt], 0, 0, 0);
+          pk[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, pb, pk[mt], 0, 0, 0);
         }
       }
     }
@@ -372,79 +391,93 @@ __global__ void __launch_bounds__(256) rel_mfma_dq_kernel(RelArgs a, const bf16_
   }
 }
 
-// ---- backward: dk and dv -----------------------------------------------------------------------------------------------------
+// ---- backward: dk and dv, and dx of every pair summed over images ----------------------------------------------------------------
+// A workgroup has the keys of its part for a head of every `splits`-th image, one after the other.  Where the table learns, each wavefront adds dx of its keys
+// to pairs [splits][heads][NT keys][NT queries][4][64][4]: a tile's sums so far come in while its scores are formed; they are a wavefront's own, in
+// the caches, so the sum over images has one order and needs no atomics.
 template <int DH, bool BIAS, bool DROP>
-__global__ void __launch_bounds__(256) rel_mfma_dkv_kernel(RelArgs a, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ d_o, const float* __restrict__ rows,
-                                                           bf16_t* __restrict__ dqkv, int parts) {
+__global__ void __launch_bounds__(256, DH <= 64 ? 2 : 1) rel_mfma_dkv_kernel(RelArgs a, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ d_o,
+                                                                             const float* __restrict__ rows, bf16_t* __restrict__ dqkv, float* pairs, int parts,
+                                                                             int splits) {
   using D = Dim<DH>;
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int STAGE = D::STAGE + 3 * KB * 4;
-  int bh, part;
-  if (!head_part(a.B * a.heads, parts, &bh, &part)) return;
+  int sh, part;
+  if (!head_part(splits * a.heads, parts, &sh, &part)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = blockDim.x >> 6, h = lane >> 5;
-  const int b = bh / a.heads, head = bh - b * a.heads, d = a.heads * DH, n = rel_tokens(a, b);
+  const int split = sh / a.heads, head = sh - split * a.heads, d = a.heads * DH;
   const size_t ld = 3 * (size_t)d;
   const int u0 = (part * waves + wave) * 32, u = u0 + (lane & 31), first = part * waves * 32;
-  const bf16_t* base = qkv + (size_t)b * a.T * ld + head * DH;
-  f32x16_t dk[D::NM], dv[D::NM];
-#pragma unroll
-  for (int mt = 0; mt < D::NM; ++mt) dk[mt] = dv[mt] = zero16();
-  if (first < n) {
-    float* table = reinterpret_cast<float*>(smem + 2 * STAGE);
-    Stager<DH> st;
-    st.init(base, d_o + (size_t)b * a.T * d + head * DH, (unsigned)ld * 2, (unsigned)d * 2, n, lane);
-    const i32x4_t rs = make_desc(rows + (size_t)bh * 3 * a.Tp, (unsigned)a.Tp * 12u);
-    auto load = [&](int s) __attribute__((always_inline)) {
-      const unsigned to = (s & 1) * STAGE;
-      st.load(s * KB, to, wave, waves);
-      for (int k = waves - 1 - wave; k < 3; k += waves) load4_to_lds(rs, to + D::STAGE + k * KB * 4, (unsigned)(k * a.Tp + s * KB + lane) * 4u);
-    };
-    load(0);
-    const unsigned short* map = nullptr;
-    MapRegs mr, next;
+  float* table = reinterpret_cast<float*>(smem + 2 * STAGE);
+  if (BIAS) table_put(table, a, head);
+  RelKey key{0u, 0u};
+  if (DROP) key = rel_key(a.rng, a.site);
+  const unsigned short* map = BIAS ? a.by_key + (size_t)(u0 >> 5) * a.NT * 1024 : nullptr;
+  float* sums = BIAS && pairs ? pairs + (((size_t)split * a.heads + head) * a.NT + (u0 >> 5)) * a.NT * 1024 + lane * 4 : nullptr;
+  for (int b = split; b < a.B; b += splits) {
+    const int n = rel_tokens(a, b), bh = b * a.heads + head;
+    const bf16_t* base = qkv + (size_t)b * a.T * ld + head * DH;
+    const int tiles = first < n ? (n + 31) >> 5 : 0;
     const bool mine = u0 < n;
-    if (BIAS) {
-      if (mine) {
-        map = a.by_key + (size_t)(u0 >> 5) * a.NT * 1024;
-        map_load(next, map, 0, a.NT - 1, lane);
-      }
-      table_put(table, a, head);
-    }
-    bf16x8_t bk[D::NK], bv[D::NK];
-    own_frags<D::NK>(base + d, ld, u, n, h, bk);
-    own_frags<D::NK>(base + 2 * d, ld, u, n, h, bv);
-    RelKey key{0u, 0u};
-    if (DROP) key = rel_key(a.rng, a.site);
-    const int stages = (n + KB - 1) / KB;
-    for (int s = 0; s < stages; ++s) {
-      wait_vm<0>();
-      workgroup_barrier();
-      mr = next;
-      if (s + 1 < stages) {
-        load(s + 1);
-        if (BIAS && mine) map_load(next, map, 2 * (s + 1), a.NT - 1, lane);
-      }
-      const unsigned char *Qs = smem + (s & 1) * STAGE, *Gs = Qs + D::MAT;
-      const float* R = reinterpret_cast<const float*>(Qs + D::STAGE);
+    f32x16_t dk[D::NM], dv[D::NM];
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int t0 = s * KB + half * 32;
-        if (!mine || t0 >= n) break;
-        f32x16_t p = tile_nt<D::NK>(Qs, D::PLANE, half * 32, bk, lane);
-        f32x16_t dx = tile_nt<D::NK>(Gs, D::PLANE, half * 32, bv, lane);
+    for (int mt = 0; mt < D::NM; ++mt) dk[mt] = dv[mt] = zero16();
+    if (tiles) {
+      if (b != split) workgroup_barrier();       // the image before is read
+      Stager<DH> st;
+      st.init(base, d_o + (size_t)b * a.T * d + head * DH, (unsigned)ld * 2, (unsigned)d * 2, n, lane);
+      const i32x4_t rs = make_desc(rows + (size_t)bh * 3 * a.Tp, (unsigned)a.Tp * 12u);
+      auto load = [&](int s) __attribute__((always_inline)) {
+        const unsigned to = (s & 1) * STAGE;
+        st.load(s * KB, to, wave, waves);
+        for (int k = waves - 1 - wave; k < 3; k += waves) load4_to_lds(rs, to + D::STAGE + k * KB * 4, (unsigned)(k * a.Tp + s * KB + lane) * 4u);
+      };
+      load(0);
+      MapRegs mr, next;
+      if (BIAS && mine) map_load(next, map, 0, lane);
+      bf16x8_t bk[D::NK], bv[D::NK];
+      own_frags<D::NK>(base + d, ld, u, n, h, bk);
+      scale_frags<DH>(bk);
+      own_frags<D::NK>(base + 2 * d, ld, u, n, h, bv);
+      for (int t = 0; t < tiles; ++t) {
+        if ((t & 1) == 0) {
+          // The loads of this stage are followed by at least the eight stores of the tiles before where there are sums.
+          asm volatile("" ::: "memory");
+          if (t && sums && mine) wait_vm<8>();
+          else wait_vm<0>();
+          workgroup_barrier();
+          if (t + 2 < tiles) load((t >> 1) + 1);
+        }
+        if (!mine) continue;
+        if (BIAS) {
+          mr = next;
+          if (t + 1 < tiles) map_load(next, map, t + 1, lane);
+        }
+        float4 was[4];
+        if (BIAS && sums) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) was[k] = float4{0.f, 0.f, 0.f, 0.f};
+          if (b != split) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) was[k] = *reinterpret_cast<const float4*>(sums + (size_t)t * 1024 + k * 256);
+          }
+        }
+        const unsigned char *S = smem + (t >> 1 & 1) * STAGE, *Qs = S + (t & 1) * 32 * ROW_B, *Gs = Qs + D::MAT;
+        const float* R = reinterpret_cast<const float*>(S + D::STAGE) + (t & 1) * 32;
+        f32x16_t p = score_tile<DH, BIAS>(Qs, bk, table, mr, a.scale, lane);
+        f32x16_t dx = tile_nt<D::NK>(Gs, D::PLANE, 0, bv, lane);
         unsigned word[16];
-        if (DROP) draws_by_key(word, t0, (unsigned)u >> 1, (unsigned)bh, key, lane);
+        if (DROP) draws_by_key(word, t * 32, (unsigned)u >> 1, (unsigned)bh, key, lane);
         const unsigned q16 = a.dr.q << 16;
 #pragma unroll
         for (int i4 = 0; i4 < 4; ++i4) {
-          const float* r = R + half * 32 + i4 * 8 + h * 4;
+          const float* r = R + i4 * 8 + h * 4;
           const float4 m4 = *reinterpret_cast<const float4*>(r), l4 = *reinterpret_cast<const float4*>(r + KB), d4 = *reinterpret_cast<const float4*>(r + 2 * KB);
           const float mm[4] = {m4.x, m4.y, m4.z, m4.w}, ll[4] = {l4.x, l4.y, l4.z, l4.w}, dd[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             const int i = i4 * 4 + k;
-            const float xi = BIAS ? fmaf(p[i], a.scale, bias_of(reinterpret_cast<const unsigned char*>(table), mr.v + 2 * half, i)) : p[i] * a.scale;
-            const float pp = __builtin_amdgcn_exp2f(fmaf(xi - mm[k], kLog2e, -ll[k]));
+            const float pp = __builtin_amdgcn_exp2f(fmaf(p[i] - mm[k], kLog2e, -ll[k]));
             if (DROP) {
               const bool gone = word[i] < q16;
               p[i] = gone ? 0.f : pp;
@@ -455,114 +488,44 @@ __global__ void __launch_bounds__(256) rel_mfma_dkv_kernel(RelArgs a, const bf16
             }
           }
         }
+        if (BIAS && sums) {
+          if (u0 + 32 > n) {       // keys past the image's tokens: probabilities that may be infinite
+#pragma unroll
+            for (int i = 0; i < 16; ++i) dx[i] = u < n ? dx[i] : 0.f;
+          }
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            *reinterpret_cast<float4*>(sums + (size_t)t * 1024 + k * 256) =
+                float4{was[k].x + dx[4 * k], was[k].y + dx[4 * k + 1], was[k].z + dx[4 * k + 2], was[k].w + dx[4 * k + 3]};
+        }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           const bf16x8_t pb = pack_frag(p, j), db = pack_frag(dx, j);
 #pragma unroll
           for (int mt = 0; mt < D::NM; ++mt) {
-            dv[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_read_tr(Gs, D::PLANE, mt, half * 32 + 16 * j, lane), pb, dv[mt], 0, 0, 0);
-            dk[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_read_tr(Qs, D::PLANE, mt, half * 32 + 16 * j, lane), db, dk[mt], 0, 0, 0);
+            dv[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_read_tr(Gs, D::PLANE, mt, 16 * j, lane), pb, dv[mt], 0, 0, 0);
+            dk[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_read_tr(Qs, D::PLANE, mt, 16 * j, lane), db, dk[mt], 0, 0, 0);
           }
         }
       }
     }
-  }
-  if (u0 >= a.T) return;
-  const float up = DROP ? a.dr.scale : 1.f;
+    if (u0 >= a.T) continue;
+    if (BIAS && sums && b == split) {      // blocks that this image has no pairs in
+      for (int t = mine ? tiles : 0; t < a.NT; ++t)
 #pragma unroll
-  for (int mt = 0; mt < D::NM; ++mt)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      dk[mt][i] = u < n ? dk[mt][i] * a.scale : 0.f;
-      dv[mt][i] = u < n ? dv[mt][i] * up : 0.f;
+        for (int k = 0; k < 4; ++k) *reinterpret_cast<float4*>(sums + (size_t)t * 1024 + k * 256) = float4{0.f, 0.f, 0.f, 0.f};
     }
-  bf16_t* out = dqkv + (size_t)b * a.T * ld + head * DH + d + (size_t)u * ld;
-  store_cols<DH>(out, dk, h, u < a.T);
-  store_cols<DH>(out + d, dv, h, u < a.T);
-}
-
-// ---- backward: dx of every pair summed over images -----------------------------------------------------------------------------
-// A workgroup has the pairs of 128 queries (32 a wavefront) and 64 keys of a head for every `splits`-th image; the sums stay in
-// registers.  pairs [splits][heads][NT][NT][64][16] in the order of by_query.
-template <int DH, bool DROP>
-__global__ void __launch_bounds__(256) rel_mfma_pairs_kernel(RelArgs a, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ d_o, const float* __restrict__ rows,
-                                                             float* __restrict__ pairs, int splits) {
-  using D = Dim<DH>;
-  extern __shared__ __align__(16) unsigned char smem[];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), h = lane >> 5, d = a.heads * DH;
-  const int groups = (a.NT + 3) / 4, stages = (a.NT + 1) / 2;
-  int g = blockIdx.x;
-  const int head = g % a.heads;
-  g /= a.heads;
-  const int stage = g % stages;
-  g /= stages;
-  const int group = g % groups, split = g / groups;
-  const size_t ld = 3 * (size_t)d;
-  const int q0 = (group * 4 + wave) * 32, q = q0 + (lane & 31), k0 = stage * KB;
-  const bool mine = q0 < a.T;
-  float* table = reinterpret_cast<float*>(smem + 2 * D::STAGE);
-  f32x16_t sum[2] = {zero16(), zero16()};
-  MapRegs mr;
-  if (mine) map_load(mr, a.by_query + (size_t)(q0 >> 5) * a.NT * 1024, 2 * stage, a.NT - 1, lane);
-  table_put(table, a, head);
-  RelKey key{0u, 0u};
-  if (DROP) key = rel_key(a.rng, a.site);
-  bf16x8_t bq[D::NK], bg[D::NK], nq[D::NK], ng[D::NK];
-  float m = 0.f, L2 = 0.f, delta = 0.f, nm = 0.f, nL2 = 0.f, nd = 0.f;
-  auto fetch = [&](int b, int to) __attribute__((always_inline)) {
-    const int n = rel_tokens(a, b);
-    const bf16_t* base = qkv + (size_t)b * a.T * ld + head * DH;
-    Stager<DH> st;
-    st.init(base + d, base + 2 * d, (unsigned)ld * 2, (unsigned)ld * 2, n, lane);
-    st.load(k0, to * D::STAGE, wave, 4);
-    own_frags<D::NK>(base, ld, q, n, h, nq);
-    own_frags<D::NK>(d_o + (size_t)b * a.T * d + head * DH, d, q, n, h, ng);
-    const float* r = rows + (size_t)(b * a.heads + head) * 3 * a.Tp + q;
-    nm = 0.f, nL2 = INFINITY, nd = 0.f;
-    if (q < n) nm = r[0], nL2 = r[a.Tp], nd = r[2 * a.Tp];
-  };
-  if (split < a.B) fetch(split, 0);
-  int to = 0;
-  for (int b = split; b < a.B; b += splits, to ^= 1) {
-    wait_vm<0>();
-    workgroup_barrier();
+    const float up = DROP ? a.dr.scale : 1.f;
 #pragma unroll
-    for (int k = 0; k < D::NK; ++k) bq[k] = nq[k], bg[k] = ng[k];
-    m = nm, L2 = nL2, delta = nd;
-    if (b + splits < a.B) fetch(b + splits, to ^ 1);
-    const int n = rel_tokens(a, b);
-    const unsigned char *Ks = smem + to * D::STAGE, *Vs = Ks + D::MAT;
-    if (q0 >= n) continue;
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int kk = k0 + half * 32;
-      if (kk >= n) break;
-      const f32x16_t x = tile_nt<D::NK>(Ks, D::PLANE, half * 32, bq, lane);
-      const f32x16_t dp = tile_nt<D::NK>(Vs, D::PLANE, half * 32, bg, lane);
-      unsigned word[8];
-      if (DROP) draws_by_query(word, kk, (unsigned)q >> 2, (unsigned)(b * a.heads + head), key, lane);
-      const unsigned q16 = a.dr.q << 16;
-      const bool tail = kk + 32 > n;
+    for (int mt = 0; mt < D::NM; ++mt)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const float xi = fmaf(x[i], a.scale, bias_of(reinterpret_cast<const unsigned char*>(table), mr.v + 2 * half, i));
-        const float p = __builtin_amdgcn_exp2f(fmaf(xi - m, kLog2e, -L2));
-        float w = 1.f;
-        if (DROP) w = (i & 1 ? word[i >> 1] : word[i >> 1] << 16) < q16 ? 0.f : a.dr.scale;
-        float dx = p * (DROP ? fmaf(dp[i], w, -delta) : dp[i] - delta);
-        if (tail && kk + key_of(i, h) >= n) dx = 0.f;
-        sum[half][i] += dx;
+        dk[mt][i] = u < n ? dk[mt][i] * a.scale : 0.f;
+        dv[mt][i] = u < n ? dv[mt][i] * up : 0.f;
       }
-    }
-  }
-  if (!mine) return;
-#pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    const int kt = 2 * stage + half;
-    if (kt >= a.NT) break;
-    float4* out = reinterpret_cast<float4*>(pairs + ((((size_t)split * a.heads + head) * a.NT + (q0 >> 5)) * a.NT + kt) * 1024 + lane * 16);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = float4{sum[half][4 * i], sum[half][4 * i + 1], sum[half][4 * i + 2], sum[half][4 * i + 3]};
+    bf16_t* out = dqkv + (size_t)b * a.T * ld + head * DH + d + (size_t)u * ld;
+    store_cols<DH>(out, dk, h, u < a.T);
+    store_cols<DH>(out + d, dv, h, u < a.T);
   }
 }
 
@@ -585,18 +548,12 @@ template <int DH, bool BIAS, bool DROP>
 int bwd_launch(const RelArgs& a, const bf16_t* qkv, const bf16_t* o, const bf16_t* d_o, const float* stats, bf16_t* dqkv, float* rows, float* pairs,
                int splits, hipStream_t st) {
   const int waves = a.NT < 4 ? a.NT : 4, parts = (a.NT + waves - 1) / waves, heads = a.B * a.heads;
-  const unsigned grid = (heads + 7) / 8 * 8 * parts;
   const size_t lds = 2 * Dim<DH>::STAGE + table_bytes(a), lds_kv = lds + 2 * 3 * KB * 4;
   const auto dq = rel_mfma_dq_kernel<DH, BIAS, DROP>;
   const auto dkv = rel_mfma_dkv_kernel<DH, BIAS, DROP>;
   if (allow_lds(dq, lds) != CNNK_OK || allow_lds(dkv, lds_kv) != CNNK_OK) return CNNK_ERR_HIP;
-  dq<<<grid, 64 * waves, lds, st>>>(a, qkv, o, d_o, stats, dqkv, rows, parts);
-  dkv<<<grid, 64 * waves, lds_kv, st>>>(a, qkv, d_o, rows, dqkv, parts);
-  if (BIAS && pairs) {
-    const auto sums = rel_mfma_pairs_kernel<DH, DROP>;
-    if (allow_lds(sums, lds) != CNNK_OK) return CNNK_ERR_HIP;
-    sums<<<a.heads * ((a.NT + 1) / 2) * ((a.NT + 3) / 4) * splits, 256, lds, st>>>(a, qkv, d_o, rows, pairs, splits);
-  }
+  dq<<<(heads + 7) / 8 * 8 * parts, 64 * waves, lds, st>>>(a, qkv, o, d_o, stats, dqkv, rows, parts);
+  dkv<<<(splits * a.heads + 7) / 8 * 8 * parts, 64 * waves, lds_kv, st>>>(a, qkv, d_o, rows, dqkv, pairs, parts, splits);
   return launch_status();
 }
 template <int DH> int fwd_of(const RelArgs& a, const bf16_t* qkv, bf16_t* o, float* stats, hipStream_t st) {
@@ -618,7 +575,7 @@ int rel_mfma_fwd(const RelArgs& a, const void* qkv, void* o, float* stats, hipSt
   const bf16_t* x = (const bf16_t*)qkv;
   bf16_t* y = (bf16_t*)o;
   return a.dh == 16 ? fwd_of<16>(a, x, y, stats, st) : a.dh == 32 ? fwd_of<32>(a, x, y, stats, st) : a.dh == 64 ? fwd_of<64>(a, x, y, stats, st)
-                                                                                                                 : fwd_of<128>(a, x, y, stats, st);
+                                                                                                           : fwd_of<128>(a, x, y, stats, st);
 }
 int rel_mfma_bwd(const RelArgs& a, const void* qkv, const void* o, const void* d_o, const float* stats, void* dqkv, float* rows, float* pairs, int splits,
                  hipStream_t st) {

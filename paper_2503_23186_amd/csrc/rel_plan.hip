@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(64) plan_list_kernel(int T, int NT, int pairs,
     __syncthreads();
     if (k >= 0) {
       const int t = i / T, u = i - t * T;
-      list[place] = ((t >> 5) * NT + (u >> 5)) * 1024 + rel_place(u & 31, t & 31);
+      list[place] = rel_sum_place(NT, t, u);
       if (before == all - 1) at[k] = place + 1;
     }
     __syncthreads();

@@ -157,9 +157,9 @@ def test_plans_are_reproducible_and_ignore_what_they_overwrite(K):
     lists = [x[at:at + 4 * int(start[-1])].view(torch.int32) for x in (a, b)]
     assert torch.equal(lists[0], lists[1]) and torch.equal(a[:maps], b[:maps])
     order = lists[0].cpu().numpy()
-    block, place = order >> 10, order & 1023
-    lane, reg = place >> 4, place & 15
-    t, u = block // NT * 32 + (lane & 31), block % NT * 32 + (reg >> 2) * 8 + (lane >> 5) * 4 + (reg & 3)
+    block, place = order >> 10, order & 1023                     # blocks of keys, in them of queries; [4][64 lanes][4] of a block
+    lane, reg = place >> 2 & 63, (place >> 8) * 4 + (place & 3)
+    t, u = block % NT * 32 + (reg >> 2) * 8 + (lane >> 5) * 4 + (reg & 3), block // NT * 32 + (lane & 31)
     assert (t * T + u == np.concatenate([np.flatnonzero(ids == k) for k in range(n)])).all()
 
 
