@@ -1,4 +1,4 @@
-// What the attention kernels behind include/cnnk_rel.h get: the general ones (rel_attention.hip) and those on the matrix cores (rel_attention_mfma.hip).
+// What the attention kernels behind include/cnnk_rel.h get (rel_attention_mfma.h), and how the entry points (rel_attention.hip) reach them.
 #pragma once
 #include "rel.h"
 
@@ -19,7 +19,7 @@ __device__ __forceinline__ int rel_tokens(const RelArgs& a, int b) {
   return n < 0 ? 0 : n > a.T ? a.T : n;
 }
 
-// bf16 storage.  rows: [B * heads][3][Tp] floats, pairs (NULL: no gradient of the table): [splits][heads][NT][NT][1024]
-int rel_mfma_fwd(const RelArgs& a, const void* qkv, void* o, float* stats, hipStream_t st);
-int rel_mfma_bwd(const RelArgs& a, const void* qkv, const void* o, const void* d_o, const float* stats, void* dqkv, float* rows, float* pairs, int splits,
-                 hipStream_t st);
+// rows: [B * heads][3][Tp] floats; pairs (NULL: no gradient of the table): [splits][heads][NT][NT][1024].  T: bf16_t or float
+template <typename T> int rel_mfma_fwd(const RelArgs& a, const T* qkv, T* o, float* stats, hipStream_t st);
+template <typename T>
+int rel_mfma_bwd(const RelArgs& a, const T* qkv, const T* o, const T* d_o, const float* stats, T* dqkv, float* rows, float* pairs, int splits, hipStream_t st);

@@ -1,7 +1,7 @@
-// Self-attention with a learned relative position bias, dropout of the probabilities and padded batches on the matrix cores (bf16 storage, head
-// sizes 16, 32, 64, 128, any number of tokens): forward, gradients of q, k and v, gradient of the bias table.
+// Self-attention with a learned relative position bias, dropout of the probabilities and padded batches on the matrix cores (head sizes
+// 16, 32, 64, 128, any number of tokens; bf16 storage on v_mfma_f32_32x32x16_bf16, fp32 on v_mfma_f32_32x32x2_f32): forward, gradients of q, k and v, gradient of the bias table.
 //
-// A wavefront owns 32 queries (keys) and walks over the keys (queries), which come into LDS 64 at a time by direct loads, two buffers: one
+// A wavefront owns 32 queries (keys) and walks over the keys (queries), which come into LDS 64 (fp32: 32) at a time by direct loads, two buffers: one
 // barrier a stage, the loads of a stage under the products of the one before.  Rows past an image's tokens are out of the loads' range and
 // arrive as zeros.  Score tiles as in vit_attention_mfma.hip: rows = keys, columns = queries in the forward pass and for dq, so that a
 // query's statistics are a lane's own and the accumulator is the next product's operand; the other way round for dk and dv.
@@ -19,45 +19,158 @@
 // Dropout: a call of the generator gives eight draws, of four queries and two keys (include/cnnk_rel.h).  With a query a lane, four neighbouring
 // lanes need the four words of the same calls: each makes a quarter of the calls and they transpose words among
 // themselves; with a key a lane, two neighbours share a call, and each makes half of them.
+#pragma once
 #include "rel_attention.h"
 #include "attn_tile.h"
 #include "mfma_tile.h"
 
 namespace {
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
-constexpr int KB = 64;               // rows of a stage
 // Probabilities are summed as 2^((x - m) log2 e - kDown), where m is a reference that a row's largest score so far passes by at most kSlack:
 // none is above 2^-14, so that sums over 16384 keys stay below the largest value.
 constexpr float kSlack = 5.5f, kDown = 22.f;
 
-template <int DH> struct Dim {
-  static constexpr int NK = DH / 16, NM = (DH + 31) / 32;
-  static constexpr int PLANE = KB * ROW_B, MAT = NM * PLANE, STAGE = 2 * MAT;
-  static constexpr bool EXACT = DH == 16 || DH == 64;      // 1 / sqrt(DH) is a power of two
+// ---- storage types -----------------------------------------------------------------------------------------------------------
+// Dim<T, DH>: the LDS layout of a stage's two matrices and the products with them.  EXACT: 1 / sqrt(DH) goes into one operand without a rounding that
+// counts (a power of two, or fp32).
+// A matrix in LDS has planes of 32 features.  bf16: attn_tile.h.  fp32: rows of 128 bytes in eight chunks of 16; in a pair of rows (256 bytes, all banks)
+// chunk c of row r lies at ((r & 1) ^ (r >> 2 & 1)) * 8 + (c ^ (r >> 1 & 7)), so that sixteen rows read at one chunk, and rows r and r + 4 read whole, touch
+// every bank once.
+template <typename T, int DH> struct Dim;
+
+template <int DH> struct Dim<bf16_t, DH> {
+  static constexpr int NK = DH / 16, NM = (DH + 31) / 32, KB = 64;      // KB: rows of a stage
+  static constexpr int PLANE = KB * ROW_B, MAT = NM * PLANE, STAGE = 2 * MAT, LOAD_ROWS = 16;
+  static constexpr bool EXACT = DH == 16 || DH == 64;
+  struct Own { bf16x8_t f[NK]; };      // 32 rows of a matrix as an operand, a row a lane
+  // which row and byte of it a lane fetches in a load of 16 rows of a plane
+  static __device__ __forceinline__ int load_row(int lane) { return lane >> 2; }
+  static __device__ __forceinline__ int load_byte(int lane, int) { return ((lane & 3) ^ (lane >> 4 & 3)) * 16; }
+  static __device__ __forceinline__ void own(const bf16_t* src, size_t ld, int row, int n, int h, Own& o) { own_frags<NK>(src, ld, row, n, h, o.f); }
+  static __device__ __forceinline__ float dot(const Own& a, const Own& b) {
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < NK; ++k) s += dot8(__builtin_bit_cast(uint4, a.f[k]), __builtin_bit_cast(uint4, b.f[k]));
+    return s;
+  }
+  static __device__ __forceinline__ void scale(Own& o) {
+    if (!EXACT) return;
+#pragma unroll
+    for (int k = 0; k < NK; ++k) {
+      float v[8];
+      unpack8(__builtin_bit_cast(uint4, o.f[k]), v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] *= DH == 64 ? 0.125f : 0.25f;
+      o.f[k] = __builtin_bit_cast(bf16x8_t, uint4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])});
+    }
+  }
+  // acc + M Own^T: rows of M by own rows
+  static __device__ __forceinline__ f32x16_t nt(const unsigned char* m, const Own& o, f32x16_t acc, int lane) {
+#pragma unroll
+    for (int k = 0; k < NK; ++k) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_read(m, PLANE, lane & 31, k * 16 + (lane >> 5) * 8), o.f[k], acc, 0, 0, 0);
+    return acc;
+  }
+  // acc += M^T x, and acc2 += M^T y: features by own rows
+  template <bool TWO> static __device__ __forceinline__ void tn(const unsigned char* m, const f32x16_t& x, const f32x16_t& y, f32x16_t* acc, f32x16_t* acc2, int lane) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const bf16x8_t xb = pack_frag(x, j), yb = TWO ? pack_frag(y, j) : xb;
+#pragma unroll
+      for (int mt = 0; mt < NM; ++mt) {
+        const bf16x8_t v = frag_read_tr(m, PLANE, mt, 16 * j, lane);
+        acc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, xb, acc[mt], 0, 0, 0);
+        if (TWO) acc2[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, yb, acc2[mt], 0, 0, 0);
+      }
+    }
+  }
+  static __device__ __forceinline__ void store(bf16_t* row, const f32x16_t* acc, int h, bool inside) { store_cols<DH>(row, acc, h, inside); }
 };
 
-// ---- stages: rows r0 .. r0 + 63 of two matrices ------------------------------------------------------------------------
-// A wavefront's direct load fills 16 rows of a plane; lane / 4 is the row and lane % 4 the place in it, whose chunk the swizzle gives.
-template <int DH> struct Stager {
+template <int DH> struct Dim<float, DH> {
+  static constexpr int NM = (DH + 31) / 32, NG = DH / 8, KB = 32;
+  static constexpr int PLANE = KB * 128, MAT = NM * PLANE, STAGE = 2 * MAT, LOAD_ROWS = 8;
+  static constexpr bool EXACT = true;
+  struct Own { float4 f[NG]; };        // features 8 g + 4 h ..  + 3 of lane half h
+  static __device__ __forceinline__ int load_row(int lane) { return (lane >> 4) * 2 + ((lane >> 3 & 1) ^ (lane >> 5)); }
+  static __device__ __forceinline__ int load_byte(int lane, int group) { return ((lane & 7) ^ ((group & 1) * 4 + (lane >> 4))) * 16; }
+  static __device__ __forceinline__ int at(int row, int chunk) {
+    return (row >> 1) * 256 + (((row & 1) ^ (row >> 2 & 1)) << 7) + ((chunk ^ (row >> 1 & 7)) << 4);
+  }
+  static __device__ __forceinline__ void own(const float* src, size_t ld, int row, int n, int h, Own& o) {
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      o.f[g] = float4{0.f, 0.f, 0.f, 0.f};
+      if (row < n) o.f[g] = *reinterpret_cast<const float4*>(src + (size_t)row * ld + g * 8 + h * 4);
+    }
+  }
+  static __device__ __forceinline__ float dot(const Own& a, const Own& b) {
+    float s = 0.f;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) s += (a.f[g].x * b.f[g].x + a.f[g].y * b.f[g].y) + (a.f[g].z * b.f[g].z + a.f[g].w * b.f[g].w);
+    return s;
+  }
+  static __device__ __forceinline__ void scale(Own& o) {
+    constexpr float s = DH == 16 ? 0.25f : DH == 32 ? 0.17677669529663689f : DH == 64 ? 0.125f : 0.088388347648318447f;
+#pragma unroll
+    for (int g = 0; g < NG; ++g) o.f[g] = float4{o.f[g].x * s, o.f[g].y * s, o.f[g].z * s, o.f[g].w * s};
+  }
+  static __device__ __forceinline__ f32x16_t nt(const unsigned char* m, const Own& o, f32x16_t acc, int lane) {
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+      const float4 v = *reinterpret_cast<const float4*>(m + (g >> 2) * PLANE + at(lane & 31, (g & 3) * 2 + (lane >> 5)));
+      acc = __builtin_amdgcn_mfma_f32_32x32x2f32(v.x, o.f[g].x, acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_32x32x2f32(v.y, o.f[g].y, acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_32x32x2f32(v.z, o.f[g].z, acc, 0, 0, 0);
+      acc = __builtin_amdgcn_mfma_f32_32x32x2f32(v.w, o.f[g].w, acc, 0, 0, 0);
+    }
+    return acc;
+  }
+  // A step reduces over the two rows that register i of the halves stands for, and needs no conversion.
+  template <bool TWO> static __device__ __forceinline__ void tn(const unsigned char* m, const f32x16_t& x, const f32x16_t& y, f32x16_t* acc, f32x16_t* acc2, int lane) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int row = (i >> 2) * 8 + (lane >> 5) * 4 + (i & 3);
+#pragma unroll
+      for (int mt = 0; mt < NM; ++mt) {
+        const float v = *reinterpret_cast<const float*>(m + mt * PLANE + at(row, (lane & 31) >> 2) + (lane & 3) * 4);
+        acc[mt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, x[i], acc[mt], 0, 0, 0);
+        if (TWO) acc2[mt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, y[i], acc2[mt], 0, 0, 0);
+      }
+    }
+  }
+  static __device__ __forceinline__ void store(float* row, const f32x16_t* acc, int h, bool inside) {
+#pragma unroll
+    for (int mt = 0; mt < NM; ++mt)
+#pragma unroll
+      for (int i4 = 0; i4 < 4; ++i4) {
+        if (mt * 32 + i4 * 8 >= DH) break;
+        if (inside) *reinterpret_cast<float4*>(row + mt * 32 + i4 * 8 + h * 4) = float4{acc[mt][4 * i4], acc[mt][4 * i4 + 1], acc[mt][4 * i4 + 2], acc[mt][4 * i4 + 3]};
+      }
+  }
+};
+
+// ---- stages: KB rows of two matrices -----------------------------------------------------------------------------------------
+// A wavefront's direct load fills LOAD_ROWS rows of a plane, 1 KB.
+template <typename T, int DH> struct Stager {
+  using D = Dim<T, DH>;
   i32x4_t x, y;                      // the matrices' descriptors
-  unsigned voff_x, voff_y;           // this lane's byte in row group 0, plane 0
   unsigned ld_x, ld_y;               // bytes of a row
-  __device__ __forceinline__ void init(const bf16_t* px, const bf16_t* py, unsigned ldx, unsigned ldy, int n, int lane) {
-    x = make_desc(px, n > 0 ? (unsigned)(n - 1) * ldx + DH * 2 : 0u);
-    y = make_desc(py, n > 0 ? (unsigned)(n - 1) * ldy + DH * 2 : 0u);
-    const int row = lane >> 2, chunk = (lane & 3) ^ (row >> 2 & 3);
-    voff_x = row * ldx + chunk * 16;
-    voff_y = row * ldy + chunk * 16;
+  int lane;
+  __device__ __forceinline__ void init(const T* px, const T* py, unsigned ldx, unsigned ldy, int n, int ln) {
+    x = make_desc(px, n > 0 ? (unsigned)(n - 1) * ldx + DH * sizeof(T) : 0u);
+    y = make_desc(py, n > 0 ? (unsigned)(n - 1) * ldy + DH * sizeof(T) : 0u);
     ld_x = ldx;
     ld_y = ldy;
+    lane = ln;
   }
   __device__ __forceinline__ void load(int r0, unsigned lds, int wave, int waves) const {
-    constexpr int PER = Dim<DH>::NM * 4;                  // loads of a matrix
+    constexpr int GROUPS = D::KB / D::LOAD_ROWS, PER = D::NM * GROUPS;                  // loads of a matrix
     for (int q = wave; q < 2 * PER; q += waves) {
       const bool second = q >= PER;
-      const int k = second ? q - PER : q, plane = k >> 2, group = k & 3;
-      const unsigned at = (unsigned)(r0 + group * 16) * (second ? ld_y : ld_x) + plane * 64;
-      load16_to_lds(second ? y : x, lds + q * 1024, (second ? voff_y : voff_x) + at);
+      const int k = second ? q - PER : q, plane = k / GROUPS, group = k % GROUPS;
+      const unsigned ld = second ? ld_y : ld_x;
+      const unsigned at = (unsigned)(r0 + group * D::LOAD_ROWS + D::load_row(lane)) * ld + plane * 32 * sizeof(T) + D::load_byte(lane, group);
+      load16_to_lds(second ? y : x, lds + q * 1024, at);
     }
   }
 };
@@ -74,41 +187,27 @@ __device__ __forceinline__ float bias_of(const unsigned char* table, const MapRe
   const unsigned w = (i & 7) < 4 ? ((i & 7) < 2 ? q.x : q.y) : ((i & 7) < 6 ? q.z : q.w);
   return *reinterpret_cast<const float*>(table + (i & 1 ? w >> 16 : w & 0xffffu));
 }
-// the head's column of the table, -infinity behind it
-__device__ __forceinline__ void table_put(float* dst, const RelArgs& a, int h) {
-  for (int k = threadIdx.x; k < a.buckets; k += blockDim.x) dst[k] = a.table[(size_t)k * a.heads + h];
+// the head's column of the table, straight into LDS (there with the first stage), -infinity behind it
+__device__ __forceinline__ void table_load(unsigned lds, float* dst, const RelArgs& a, int head, int wave, int waves, int lane) {
+  const i32x4_t desc = make_desc(a.table, (unsigned)a.buckets * a.heads * 4u);
+  for (int k0 = wave * 64; k0 < a.buckets; k0 += waves * 64)
+    if (k0 + lane < a.buckets) load4_to_lds(desc, lds + k0 * 4, (unsigned)((k0 + lane) * a.heads + head) * 4u);
   if (threadIdx.x == 0) dst[a.buckets] = -INFINITY;
 }
-
-// q times 1 / sqrt(DH) where that is exact
-template <int DH> __device__ __forceinline__ void scale_frags(bf16x8_t* f) {
-  if (!Dim<DH>::EXACT) return;
-#pragma unroll
-  for (int k = 0; k < Dim<DH>::NK; ++k) {
-    float v[8];
-    unpack8(__builtin_bit_cast(uint4, f[k]), v);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] *= DH == 64 ? 0.125f : 0.25f;
-    f[k] = __builtin_bit_cast(bf16x8_t, uint4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])});
-  }
-}
-// A tile of scores with their bias.  One operand has been through scale_frags.
-template <int DH, bool BIAS>
-__device__ __forceinline__ f32x16_t score_tile(const unsigned char* a, const bf16x8_t* b, const float* table, const MapRegs& m, float scale, int lane) {
+// A tile of scores with their bias.  One operand has been through Dim::scale.
+template <typename T, int DH, bool BIAS>
+__device__ __forceinline__ f32x16_t score_tile(const unsigned char* m, const typename Dim<T, DH>::Own& o, const float* table, const MapRegs& map, float scale, int lane) {
+  using D = Dim<T, DH>;
   const unsigned char* t = reinterpret_cast<const unsigned char*>(table);
-  f32x16_t x;
-  if (BIAS && Dim<DH>::EXACT) {
+  f32x16_t x = zero16();
+  if (BIAS && D::EXACT) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = bias_of(t, m, i);
-  } else {
-    x = zero16();
+    for (int i = 0; i < 16; ++i) x[i] = bias_of(t, map, i);
   }
+  x = D::nt(m, o, x, lane);
+  if (!D::EXACT) {
 #pragma unroll
-  for (int k = 0; k < Dim<DH>::NK; ++k)
-    x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_read(a, Dim<DH>::PLANE, lane & 31, k * 16 + (lane >> 5) * 8), b[k], x, 0, 0, 0);
-  if (!Dim<DH>::EXACT) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = BIAS ? fmaf(x[i], scale, bias_of(t, m, i)) : x[i] * scale;
+    for (int i = 0; i < 16; ++i) x[i] = BIAS ? fmaf(x[i], scale, bias_of(t, map, i)) : x[i] * scale;
   }
   return x;
 }
@@ -171,10 +270,11 @@ __device__ __forceinline__ float both_halves_sum(float v) {
 __device__ __forceinline__ int key_of(int i, int h) { return (i >> 2) * 8 + h * 4 + (i & 3); }
 
 // ---- forward ---------------------------------------------------------------------------------------------------------------
-template <int DH, bool BIAS, bool DROP>
-__global__ void __launch_bounds__(256, DH <= 64 ? 3 : 2) rel_mfma_fwd_kernel(RelArgs a, const bf16_t* __restrict__ qkv, bf16_t* __restrict__ o,
+template <typename T, int DH, bool BIAS, bool DROP>
+__global__ void __launch_bounds__(512, sizeof(T) == 2 && DH <= 64 ? 3 : 2) rel_mfma_fwd_kernel(RelArgs a, const T* __restrict__ qkv, T* __restrict__ o,
                                                                              float* __restrict__ stats, int parts) {
-  using D = Dim<DH>;
+  using D = Dim<T, DH>;
+  constexpr int TS = D::KB / 32, TILE = D::PLANE / TS;      // tiles of a stage, bytes of a tile's rows in a plane
   extern __shared__ __align__(16) unsigned char smem[];
   int bh, part;
   if (!head_part(a.B * a.heads, parts, &bh, &part)) return;
@@ -182,42 +282,43 @@ __global__ void __launch_bounds__(256, DH <= 64 ? 3 : 2) rel_mfma_fwd_kernel(Rel
   const int b = bh / a.heads, head = bh - b * a.heads, d = a.heads * DH, n = rel_tokens(a, b);
   const size_t ld = 3 * (size_t)d;
   const int q0 = (part * waves + wave) * 32, q = q0 + (lane & 31), first = part * waves * 32;
-  const bf16_t* base = qkv + (size_t)b * a.T * ld + head * DH;
+  const T* base = qkv + (size_t)b * a.T * ld + head * DH;
   f32x16_t oacc[D::NM];
 #pragma unroll
   for (int mt = 0; mt < D::NM; ++mt) oacc[mt] = zero16();
   float m = -INFINITY, l = 0.f;      // l: of this lane's half of the keys
   if (first < n) {
     float* table = reinterpret_cast<float*>(smem + 2 * D::STAGE);
-    Stager<DH> st;
-    st.init(base + d, base + 2 * d, (unsigned)ld * 2, (unsigned)ld * 2, n, lane);
+    Stager<T, DH> st;
+    st.init(base + d, base + 2 * d, (unsigned)(ld * sizeof(T)), (unsigned)(ld * sizeof(T)), n, lane);
     st.load(0, 0, wave, waves);
     const bool mine = q0 < n;
     const unsigned short* map = BIAS ? a.by_query + (size_t)(q0 >> 5) * a.NT * 1024 : nullptr;
     MapRegs mr, next;
     if (BIAS) {
       if (mine) map_load(next, map, 0, lane);
-      table_put(table, a, head);
+      table_load(2 * D::STAGE, table, a, head, wave, waves, lane);
     }
-    bf16x8_t bq[D::NK];
-    own_frags<D::NK>(base, ld, q, n, h, bq);
-    scale_frags<DH>(bq);
+    typename D::Own bq;
+    D::own(base, ld, q, n, h, bq);
+    D::scale(bq);
     RelKey key{0u, 0u};
     if (DROP) key = rel_key(a.rng, a.site);
     const int tiles = (n + 31) >> 5;
     for (int t = 0; t < tiles; ++t) {
-      if ((t & 1) == 0) {
+      const int stage = t / TS;
+      if (t % TS == 0) {
         wait_vm<0>();
         workgroup_barrier();
-        if (t + 2 < tiles) st.load(t * 32 + KB, ((t >> 1) + 1 & 1) * D::STAGE, wave, waves);
+        if (t + TS < tiles) st.load(t * 32 + D::KB, (stage + 1 & 1) * D::STAGE, wave, waves);
       }
       if (!mine) continue;
       if (BIAS) {
         mr = next;
         if (t + 1 < tiles) map_load(next, map, t + 1, lane);
       }
-      const unsigned char *Ks = smem + (t >> 1 & 1) * D::STAGE + (t & 1) * 32 * ROW_B, *Vs = Ks + D::MAT;
-      f32x16_t x = score_tile<DH, BIAS>(Ks, bq, table, mr, a.scale, lane);
+      const unsigned char *Ks = smem + (stage & 1) * D::STAGE + t % TS * TILE, *Vs = Ks + D::MAT;
+      f32x16_t x = score_tile<T, DH, BIAS>(Ks, bq, table, mr, a.scale, lane);
       if (t * 32 + 32 > n) {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
@@ -255,13 +356,7 @@ __global__ void __launch_bounds__(256, DH <= 64 ? 3 : 2) rel_mfma_fwd_kernel(Rel
           x[2 * j + 1] = word[j] < q16 ? 0.f : x[2 * j + 1];
         }
       }
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const bf16x8_t pb = pack_frag(x, j);
-#pragma unroll
-        for (int mt = 0; mt < D::NM; ++mt)
-          oacc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_read_tr(Vs, D::PLANE, mt, 16 * j, lane), pb, oacc[mt], 0, 0, 0);
-      }
+      D::template tn<false>(Vs, x, x, oacc, oacc, lane);
     }
   }
   if (q0 >= a.T) return;
@@ -272,7 +367,7 @@ __global__ void __launch_bounds__(256, DH <= 64 ? 3 : 2) rel_mfma_fwd_kernel(Rel
   for (int mt = 0; mt < D::NM; ++mt)
 #pragma unroll
     for (int i = 0; i < 16; ++i) oacc[mt][i] = any ? oacc[mt][i] * inv : 0.f;
-  store_cols<DH>(o + ((size_t)b * a.T + q) * d + head * DH, oacc, h, q < a.T);
+  D::store(o + ((size_t)b * a.T + q) * d + head * DH, oacc, h, q < a.T);
   if (stats && h == 0 && q < a.T)
     *reinterpret_cast<float2*>(stats + ((size_t)bh * a.T + q) * 2) = any ? float2{m, kLn2 * (__builtin_amdgcn_logf(l) + kDown)} : float2{-INFINITY, 0.f};
 }
@@ -280,11 +375,12 @@ __global__ void __launch_bounds__(256, DH <= 64 ? 3 : 2) rel_mfma_fwd_kernel(Rel
 // ---- backward: dq, and for the kernel behind it the rows' statistics and delta -----------------------------------------------
 // rows [B * heads][3][Tp], Tp = T rounded up to 64: reference, log2 of the sum relative to it (+infinity for rows without a part: their probabilities
 // come out as 0), delta.
-template <int DH, bool BIAS, bool DROP>
-__global__ void __launch_bounds__(256, DH <= 64 ? 2 : 1) rel_mfma_dq_kernel(RelArgs a, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ o,
-                                                                            const bf16_t* __restrict__ d_o, const float* __restrict__ stats,
-                                                                            bf16_t* __restrict__ dqkv, float* __restrict__ rows, int parts) {
-  using D = Dim<DH>;
+template <typename T, int DH, bool BIAS, bool DROP>
+__global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mfma_dq_kernel(RelArgs a, const T* __restrict__ qkv, const T* __restrict__ o,
+                                                                            const T* __restrict__ d_o, const float* __restrict__ stats,
+                                                                            T* __restrict__ dqkv, float* __restrict__ rows, int parts) {
+  using D = Dim<T, DH>;
+  constexpr int TS = D::KB / 32, TILE = D::PLANE / TS;      // tiles of a stage, bytes of a tile's rows in a plane
   extern __shared__ __align__(16) unsigned char smem[];
   int bh, part;
   if (!head_part(a.B * a.heads, parts, &bh, &part)) return;
@@ -292,34 +388,33 @@ __global__ void __launch_bounds__(256, DH <= 64 ? 2 : 1) rel_mfma_dq_kernel(RelA
   const int b = bh / a.heads, head = bh - b * a.heads, d = a.heads * DH, n = rel_tokens(a, b);
   const size_t ld = 3 * (size_t)d;
   const int q0 = (part * waves + wave) * 32, q = q0 + (lane & 31), first = part * waves * 32;
-  const bf16_t* base = qkv + (size_t)b * a.T * ld + head * DH;
+  const T* base = qkv + (size_t)b * a.T * ld + head * DH;
   const size_t head0 = (size_t)b * a.T * d + head * DH;
-  f32x16_t dq[D::NM], pk[D::NM];     // dx' k, P k
+  constexpr bool FIX = sizeof(T) == 2;      // fp32: do . o is delta
+  f32x16_t dq[D::NM], pk[D::NM];            // dx' k, P k
 #pragma unroll
   for (int mt = 0; mt < D::NM; ++mt) dq[mt] = pk[mt] = zero16();
   float m = 0.f, L2 = INFINITY, delta = 0.f, lack = 0.f;
   if (first < n) {
     float* table = reinterpret_cast<float*>(smem + 2 * D::STAGE);
-    Stager<DH> st;
-    st.init(base + d, base + 2 * d, (unsigned)ld * 2, (unsigned)ld * 2, n, lane);
+    Stager<T, DH> st;
+    st.init(base + d, base + 2 * d, (unsigned)(ld * sizeof(T)), (unsigned)(ld * sizeof(T)), n, lane);
     st.load(0, 0, wave, waves);
     const bool mine = q0 < n;
     const unsigned short* map = BIAS ? a.by_query + (size_t)(q0 >> 5) * a.NT * 1024 : nullptr;
     MapRegs mr, next;
     if (BIAS) {
       if (mine) map_load(next, map, 0, lane);
-      table_put(table, a, head);
+      table_load(2 * D::STAGE, table, a, head, wave, waves, lane);
     }
-    bf16x8_t bq[D::NK], bg[D::NK];
-    own_frags<D::NK>(base, ld, q, n, h, bq);
-    scale_frags<DH>(bq);
-    own_frags<D::NK>(d_o + head0, d, q, n, h, bg);
+    typename D::Own bq, bg;
+    D::own(base, ld, q, n, h, bq);
+    D::scale(bq);
+    D::own(d_o + head0, d, q, n, h, bg);
     {
-      bf16x8_t t[D::NK];
-      own_frags<D::NK>(o + head0, d, q, n, h, t);
-#pragma unroll
-      for (int k = 0; k < D::NK; ++k) delta += dot8(__builtin_bit_cast(uint4, t[k]), __builtin_bit_cast(uint4, bg[k]));
-      delta = both_halves_sum(delta);
+      typename D::Own t;
+      D::own(o + head0, d, q, n, h, t);
+      delta = both_halves_sum(D::dot(t, bg));
     }
     if (q < n) {
       const float2 s = *reinterpret_cast<const float2*>(stats + ((size_t)bh * a.T + q) * 2);
@@ -332,19 +427,20 @@ __global__ void __launch_bounds__(256, DH <= 64 ? 2 : 1) rel_mfma_dq_kernel(RelA
     if (DROP) key = rel_key(a.rng, a.site);
     const int tiles = (n + 31) >> 5;
     for (int t = 0; t < tiles; ++t) {
-      if ((t & 1) == 0) {
+      const int stage = t / TS;
+      if (t % TS == 0) {
         wait_vm<0>();
         workgroup_barrier();
-        if (t + 2 < tiles) st.load(t * 32 + KB, ((t >> 1) + 1 & 1) * D::STAGE, wave, waves);
+        if (t + TS < tiles) st.load(t * 32 + D::KB, (stage + 1 & 1) * D::STAGE, wave, waves);
       }
       if (!mine) continue;
       if (BIAS) {
         mr = next;
         if (t + 1 < tiles) map_load(next, map, t + 1, lane);
       }
-      const unsigned char *Ks = smem + (t >> 1 & 1) * D::STAGE + (t & 1) * 32 * ROW_B, *Vs = Ks + D::MAT;
-      f32x16_t p = score_tile<DH, BIAS>(Ks, bq, table, mr, a.scale, lane);
-      f32x16_t dx = tile_nt<D::NK>(Vs, D::PLANE, 0, bg, lane);
+      const unsigned char *Ks = smem + (stage & 1) * D::STAGE + t % TS * TILE, *Vs = Ks + D::MAT;
+      f32x16_t p = score_tile<T, DH, BIAS>(Ks, bq, table, mr, a.scale, lane);
+      f32x16_t dx = D::nt(Vs, bg, zero16(), lane);
       unsigned word[8];
       if (DROP) draws_by_query(word, t * 32, (unsigned)q >> 2, (unsigned)bh, key, lane);
       const unsigned q16 = a.dr.q << 16;
@@ -360,20 +456,13 @@ __global__ void __launch_bounds__(256, DH <= 64 ? 2 : 1) rel_mfma_dq_kernel(RelA
         for (int i = 0; i < 16; ++i)
           if (t * 32 + key_of(i, h) >= n) p[i] = dx[i] = 0.f;
       }
-      float add[2] = {0.f, 0.f};
+      if (FIX) {
+        float add[2] = {0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < 16; ++i) add[i & 1] += dx[i];
-      lack += add[0] + add[1];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const bf16x8_t pb = pack_frag(p, j), db = pack_frag(dx, j);
-#pragma unroll
-        for (int mt = 0; mt < D::NM; ++mt) {
-          const bf16x8_t k = frag_read_tr(Ks, D::PLANE, mt, 16 * j, lane);
-          dq[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, db, dq[mt], 0, 0, 0);
-          pk[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k, pb, pk[mt], 0, 0, 0);
-        }
+        for (int i = 0; i < 16; ++i) add[i & 1] += dx[i];
+        lack += add[0] + add[1];
       }
+      D::template tn<FIX>(Ks, dx, p, dq, pk, lane);
     }
   }
   if (q0 >= a.T) return;
@@ -381,8 +470,8 @@ __global__ void __launch_bounds__(256, DH <= 64 ? 2 : 1) rel_mfma_dq_kernel(RelA
 #pragma unroll
   for (int mt = 0; mt < D::NM; ++mt)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) dq[mt][i] = q < n ? fmaf(-lack, pk[mt][i], dq[mt][i]) * a.scale : 0.f;
-  store_cols<DH>(dqkv + (size_t)b * a.T * ld + head * DH + (size_t)q * ld, dq, h, q < a.T);
+    for (int i = 0; i < 16; ++i) dq[mt][i] = q < n ? (FIX ? fmaf(-lack, pk[mt][i], dq[mt][i]) : dq[mt][i]) * a.scale : 0.f;
+  D::store(dqkv + (size_t)b * a.T * ld + head * DH + (size_t)q * ld, dq, h, q < a.T);
   if (h == 0) {
     float* r = rows + (size_t)bh * 3 * a.Tp + q;
     r[0] = m;
@@ -395,13 +484,14 @@ __global__ void __launch_bounds__(256, DH <= 64 ? 2 : 1) rel_mfma_dq_kernel(RelA
 // A workgroup has the keys of its part for a head of every `splits`-th image, one after the other.  Where the table learns, each wavefront adds dx of its keys
 // to pairs [splits][heads][NT keys][NT queries][4][64][4]: a tile's sums so far come in while its scores are formed; they are a wavefront's own, in
 // the caches, so the sum over images has one order and needs no atomics.
-template <int DH, bool BIAS, bool DROP>
-__global__ void __launch_bounds__(256, DH <= 64 ? 2 : 1) rel_mfma_dkv_kernel(RelArgs a, const bf16_t* __restrict__ qkv, const bf16_t* __restrict__ d_o,
-                                                                             const float* __restrict__ rows, bf16_t* __restrict__ dqkv, float* pairs, int parts,
+template <typename T, int DH, bool BIAS, bool DROP>
+__global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mfma_dkv_kernel(RelArgs a, const T* __restrict__ qkv, const T* __restrict__ d_o,
+                                                                             const float* __restrict__ rows, T* __restrict__ dqkv, float* pairs, int parts,
                                                                              int splits) {
-  using D = Dim<DH>;
+  using D = Dim<T, DH>;
+  constexpr int TS = D::KB / 32, TILE = D::PLANE / TS;      // tiles of a stage, bytes of a tile's rows in a plane
   extern __shared__ __align__(16) unsigned char smem[];
-  constexpr int STAGE = D::STAGE + 3 * KB * 4;
+  constexpr int STAGE = D::STAGE + 3 * D::KB * 4;
   int sh, part;
   if (!head_part(splits * a.heads, parts, &sh, &part)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = blockDim.x >> 6, h = lane >> 5;
@@ -409,14 +499,14 @@ __global__ void __launch_bounds__(256, DH <= 64 ? 2 : 1) rel_mfma_dkv_kernel(Rel
   const size_t ld = 3 * (size_t)d;
   const int u0 = (part * waves + wave) * 32, u = u0 + (lane & 31), first = part * waves * 32;
   float* table = reinterpret_cast<float*>(smem + 2 * STAGE);
-  if (BIAS) table_put(table, a, head);
+  if (BIAS) table_load(2 * STAGE, table, a, head, wave, waves, lane);
   RelKey key{0u, 0u};
   if (DROP) key = rel_key(a.rng, a.site);
   const unsigned short* map = BIAS ? a.by_key + (size_t)(u0 >> 5) * a.NT * 1024 : nullptr;
   float* sums = BIAS && pairs ? pairs + (((size_t)split * a.heads + head) * a.NT + (u0 >> 5)) * a.NT * 1024 + lane * 4 : nullptr;
   for (int b = split; b < a.B; b += splits) {
     const int n = rel_tokens(a, b), bh = b * a.heads + head;
-    const bf16_t* base = qkv + (size_t)b * a.T * ld + head * DH;
+    const T* base = qkv + (size_t)b * a.T * ld + head * DH;
     const int tiles = first < n ? (n + 31) >> 5 : 0;
     const bool mine = u0 < n;
     f32x16_t dk[D::NM], dv[D::NM];
@@ -424,29 +514,32 @@ __global__ void __launch_bounds__(256, DH <= 64 ? 2 : 1) rel_mfma_dkv_kernel(Rel
     for (int mt = 0; mt < D::NM; ++mt) dk[mt] = dv[mt] = zero16();
     if (tiles) {
       if (b != split) workgroup_barrier();       // the image before is read
-      Stager<DH> st;
-      st.init(base, d_o + (size_t)b * a.T * d + head * DH, (unsigned)ld * 2, (unsigned)d * 2, n, lane);
+      Stager<T, DH> st;
+      st.init(base, d_o + (size_t)b * a.T * d + head * DH, (unsigned)(ld * sizeof(T)), (unsigned)(d * sizeof(T)), n, lane);
       const i32x4_t rs = make_desc(rows + (size_t)bh * 3 * a.Tp, (unsigned)a.Tp * 12u);
       auto load = [&](int s) __attribute__((always_inline)) {
         const unsigned to = (s & 1) * STAGE;
-        st.load(s * KB, to, wave, waves);
-        for (int k = waves - 1 - wave; k < 3; k += waves) load4_to_lds(rs, to + D::STAGE + k * KB * 4, (unsigned)(k * a.Tp + s * KB + lane) * 4u);
+        st.load(s * D::KB, to, wave, waves);
+        if (lane < D::KB) {
+          for (int k = waves - 1 - wave; k < 3; k += waves) load4_to_lds(rs, to + D::STAGE + k * D::KB * 4, (unsigned)(k * a.Tp + s * D::KB + lane) * 4u);
+        }
       };
       load(0);
       MapRegs mr, next;
       if (BIAS && mine) map_load(next, map, 0, lane);
-      bf16x8_t bk[D::NK], bv[D::NK];
-      own_frags<D::NK>(base + d, ld, u, n, h, bk);
-      scale_frags<DH>(bk);
-      own_frags<D::NK>(base + 2 * d, ld, u, n, h, bv);
+      typename D::Own bk, bv;
+      D::own(base + d, ld, u, n, h, bk);
+      D::scale(bk);
+      D::own(base + 2 * d, ld, u, n, h, bv);
       for (int t = 0; t < tiles; ++t) {
-        if ((t & 1) == 0) {
-          // The loads of this stage are followed by at least the eight stores of the tiles before where there are sums.
+        const int stage = t / TS;
+        if (t % TS == 0) {
+          // The loads of this stage are followed by at least the four stores of each tile before where there are sums.
           asm volatile("" ::: "memory");
-          if (t && sums && mine) wait_vm<8>();
+          if (t && sums && mine) wait_vm<4 * TS>();
           else wait_vm<0>();
           workgroup_barrier();
-          if (t + 2 < tiles) load((t >> 1) + 1);
+          if (t + TS < tiles) load(stage + 1);
         }
         if (!mine) continue;
         if (BIAS) {
@@ -462,17 +555,17 @@ __global__ void __launch_bounds__(256, DH <= 64 ? 2 : 1) rel_mfma_dkv_kernel(Rel
             for (int k = 0; k < 4; ++k) was[k] = *reinterpret_cast<const float4*>(sums + (size_t)t * 1024 + k * 256);
           }
         }
-        const unsigned char *S = smem + (t >> 1 & 1) * STAGE, *Qs = S + (t & 1) * 32 * ROW_B, *Gs = Qs + D::MAT;
-        const float* R = reinterpret_cast<const float*>(S + D::STAGE) + (t & 1) * 32;
-        f32x16_t p = score_tile<DH, BIAS>(Qs, bk, table, mr, a.scale, lane);
-        f32x16_t dx = tile_nt<D::NK>(Gs, D::PLANE, 0, bv, lane);
+        const unsigned char *S = smem + (stage & 1) * STAGE, *Qs = S + t % TS * TILE, *Gs = Qs + D::MAT;
+        const float* R = reinterpret_cast<const float*>(S + D::STAGE) + t % TS * 32;
+        f32x16_t p = score_tile<T, DH, BIAS>(Qs, bk, table, mr, a.scale, lane);
+        f32x16_t dx = D::nt(Gs, bv, zero16(), lane);
         unsigned word[16];
         if (DROP) draws_by_key(word, t * 32, (unsigned)u >> 1, (unsigned)bh, key, lane);
         const unsigned q16 = a.dr.q << 16;
 #pragma unroll
         for (int i4 = 0; i4 < 4; ++i4) {
           const float* r = R + i4 * 8 + h * 4;
-          const float4 m4 = *reinterpret_cast<const float4*>(r), l4 = *reinterpret_cast<const float4*>(r + KB), d4 = *reinterpret_cast<const float4*>(r + 2 * KB);
+          const float4 m4 = *reinterpret_cast<const float4*>(r), l4 = *reinterpret_cast<const float4*>(r + D::KB), d4 = *reinterpret_cast<const float4*>(r + 2 * D::KB);
           const float mm[4] = {m4.x, m4.y, m4.z, m4.w}, ll[4] = {l4.x, l4.y, l4.z, l4.w}, dd[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
@@ -498,15 +591,8 @@ __global__ void __launch_bounds__(256, DH <= 64 ? 2 : 1) rel_mfma_dkv_kernel(Rel
             *reinterpret_cast<float4*>(sums + (size_t)t * 1024 + k * 256) =
                 float4{was[k].x + dx[4 * k], was[k].y + dx[4 * k + 1], was[k].z + dx[4 * k + 2], was[k].w + dx[4 * k + 3]};
         }
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const bf16x8_t pb = pack_frag(p, j), db = pack_frag(dx, j);
-#pragma unroll
-          for (int mt = 0; mt < D::NM; ++mt) {
-            dv[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_read_tr(Gs, D::PLANE, mt, 16 * j, lane), pb, dv[mt], 0, 0, 0);
-            dk[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_read_tr(Qs, D::PLANE, mt, 16 * j, lane), db, dk[mt], 0, 0, 0);
-          }
-        }
+        D::template tn<false>(Gs, p, p, dv, dv, lane);
+        D::template tn<false>(Qs, dx, dx, dk, dk, lane);
       }
     }
     if (u0 >= a.T) continue;
@@ -523,9 +609,9 @@ __global__ void __launch_bounds__(256, DH <= 64 ? 2 : 1) rel_mfma_dkv_kernel(Rel
         dk[mt][i] = u < n ? dk[mt][i] * a.scale : 0.f;
         dv[mt][i] = u < n ? dv[mt][i] * up : 0.f;
       }
-    bf16_t* out = dqkv + (size_t)b * a.T * ld + head * DH + d + (size_t)u * ld;
-    store_cols<DH>(out, dk, h, u < a.T);
-    store_cols<DH>(out + d, dv, h, u < a.T);
+    T* out = dqkv + (size_t)b * a.T * ld + head * DH + d + (size_t)u * ld;
+    D::store(out, dk, h, u < a.T);
+    D::store(out + d, dv, h, u < a.T);
   }
 }
 
@@ -535,54 +621,59 @@ template <typename Kern> int allow_lds(Kern kern, size_t bytes) {      // more t
 }
 size_t table_bytes(const RelArgs& a) { return a.buckets ? (size_t)(a.buckets + 1) * 4 : 0; }
 
-template <int DH, bool BIAS, bool DROP>
-int fwd_launch(const RelArgs& a, const bf16_t* qkv, bf16_t* o, float* stats, hipStream_t st) {
-  const int waves = a.NT < 4 ? a.NT : 4, parts = (a.NT + waves - 1) / waves, pairs = a.B * a.heads;
-  const size_t lds = 2 * Dim<DH>::STAGE + table_bytes(a);
-  const auto kern = rel_mfma_fwd_kernel<DH, BIAS, DROP>;
+// A workgroup's wavefronts: eight where the table takes so much LDS that a CU holds one workgroup (and the registers are there), otherwise four.
+int waves_of(const RelArgs& a, size_t lds, bool eight) {
+  const int most = eight && lds > 81920 ? 8 : 4;
+  return a.NT < most ? a.NT : most;
+}
+template <typename T, int DH, bool BIAS, bool DROP>
+int fwd_launch(const RelArgs& a, const T* qkv, T* o, float* stats, hipStream_t st) {
+  const size_t lds = 2 * Dim<T, DH>::STAGE + table_bytes(a);
+  const int waves = waves_of(a, lds, true), parts = (a.NT + waves - 1) / waves, pairs = a.B * a.heads;
+  const auto kern = rel_mfma_fwd_kernel<T, DH, BIAS, DROP>;
   if (allow_lds(kern, lds) != CNNK_OK) return CNNK_ERR_HIP;
   kern<<<(pairs + 7) / 8 * 8 * parts, 64 * waves, lds, st>>>(a, qkv, o, stats, parts);
   return launch_status();
 }
-template <int DH, bool BIAS, bool DROP>
-int bwd_launch(const RelArgs& a, const bf16_t* qkv, const bf16_t* o, const bf16_t* d_o, const float* stats, bf16_t* dqkv, float* rows, float* pairs,
-               int splits, hipStream_t st) {
-  const int waves = a.NT < 4 ? a.NT : 4, parts = (a.NT + waves - 1) / waves, heads = a.B * a.heads;
-  const size_t lds = 2 * Dim<DH>::STAGE + table_bytes(a), lds_kv = lds + 2 * 3 * KB * 4;
-  const auto dq = rel_mfma_dq_kernel<DH, BIAS, DROP>;
-  const auto dkv = rel_mfma_dkv_kernel<DH, BIAS, DROP>;
+template <typename T, int DH, bool BIAS, bool DROP>
+int bwd_launch(const RelArgs& a, const T* qkv, const T* o, const T* d_o, const float* stats, T* dqkv, float* rows, float* pairs, int splits, hipStream_t st) {
+  const size_t lds = 2 * Dim<T, DH>::STAGE + table_bytes(a), lds_kv = lds + 2 * 3 * Dim<T, DH>::KB * 4;
+  const int waves = waves_of(a, lds_kv, DH <= 64), parts = (a.NT + waves - 1) / waves, heads = a.B * a.heads;
+  const auto dq = rel_mfma_dq_kernel<T, DH, BIAS, DROP>;
+  const auto dkv = rel_mfma_dkv_kernel<T, DH, BIAS, DROP>;
   if (allow_lds(dq, lds) != CNNK_OK || allow_lds(dkv, lds_kv) != CNNK_OK) return CNNK_ERR_HIP;
   dq<<<(heads + 7) / 8 * 8 * parts, 64 * waves, lds, st>>>(a, qkv, o, d_o, stats, dqkv, rows, parts);
   dkv<<<(splits * a.heads + 7) / 8 * 8 * parts, 64 * waves, lds_kv, st>>>(a, qkv, d_o, rows, dqkv, pairs, parts, splits);
   return launch_status();
 }
-template <int DH> int fwd_of(const RelArgs& a, const bf16_t* qkv, bf16_t* o, float* stats, hipStream_t st) {
-  if (a.buckets) return a.dr.q ? fwd_launch<DH, true, true>(a, qkv, o, stats, st) : fwd_launch<DH, true, false>(a, qkv, o, stats, st);
-  return a.dr.q ? fwd_launch<DH, false, true>(a, qkv, o, stats, st) : fwd_launch<DH, false, false>(a, qkv, o, stats, st);
+template <typename T, int DH> int fwd_of(const RelArgs& a, const T* qkv, T* o, float* stats, hipStream_t st) {
+  if (a.buckets) return a.dr.q ? fwd_launch<T, DH, true, true>(a, qkv, o, stats, st) : fwd_launch<T, DH, true, false>(a, qkv, o, stats, st);
+  return a.dr.q ? fwd_launch<T, DH, false, true>(a, qkv, o, stats, st) : fwd_launch<T, DH, false, false>(a, qkv, o, stats, st);
 }
-template <int DH>
-int bwd_of(const RelArgs& a, const bf16_t* qkv, const bf16_t* o, const bf16_t* d_o, const float* stats, bf16_t* dqkv, float* rows, float* pairs,
-           int splits, hipStream_t st) {
+template <typename T, int DH>
+int bwd_of(const RelArgs& a, const T* qkv, const T* o, const T* d_o, const float* stats, T* dqkv, float* rows, float* pairs, int splits, hipStream_t st) {
   if (a.buckets)
-    return a.dr.q ? bwd_launch<DH, true, true>(a, qkv, o, d_o, stats, dqkv, rows, pairs, splits, st)
-                  : bwd_launch<DH, true, false>(a, qkv, o, d_o, stats, dqkv, rows, pairs, splits, st);
-  return a.dr.q ? bwd_launch<DH, false, true>(a, qkv, o, d_o, stats, dqkv, rows, pairs, splits, st)
-                : bwd_launch<DH, false, false>(a, qkv, o, d_o, stats, dqkv, rows, pairs, splits, st);
+    return a.dr.q ? bwd_launch<T, DH, true, true>(a, qkv, o, d_o, stats, dqkv, rows, pairs, splits, st)
+                  : bwd_launch<T, DH, true, false>(a, qkv, o, d_o, stats, dqkv, rows, pairs, splits, st);
+  return a.dr.q ? bwd_launch<T, DH, false, true>(a, qkv, o, d_o, stats, dqkv, rows, pairs, splits, st)
+                : bwd_launch<T, DH, false, false>(a, qkv, o, d_o, stats, dqkv, rows, pairs, splits, st);
 }
 }  // namespace
 
-int rel_mfma_fwd(const RelArgs& a, const void* qkv, void* o, float* stats, hipStream_t st) {
-  const bf16_t* x = (const bf16_t*)qkv;
-  bf16_t* y = (bf16_t*)o;
-  return a.dh == 16 ? fwd_of<16>(a, x, y, stats, st) : a.dh == 32 ? fwd_of<32>(a, x, y, stats, st) : a.dh == 64 ? fwd_of<64>(a, x, y, stats, st)
-                                                                                                           : fwd_of<128>(a, x, y, stats, st);
+template <typename T> int rel_mfma_fwd(const RelArgs& a, const T* qkv, T* o, float* stats, hipStream_t st) {
+  switch (a.dh) {
+    case 16: return fwd_of<T, 16>(a, qkv, o, stats, st);
+    case 32: return fwd_of<T, 32>(a, qkv, o, stats, st);
+    case 64: return fwd_of<T, 64>(a, qkv, o, stats, st);
+    default: return fwd_of<T, 128>(a, qkv, o, stats, st);
+  }
 }
-int rel_mfma_bwd(const RelArgs& a, const void* qkv, const void* o, const void* d_o, const float* stats, void* dqkv, float* rows, float* pairs, int splits,
-                 hipStream_t st) {
-  const bf16_t *x = (const bf16_t*)qkv, *y = (const bf16_t*)o, *g = (const bf16_t*)d_o;
-  bf16_t* dx = (bf16_t*)dqkv;
-  return a.dh == 16   ? bwd_of<16>(a, x, y, g, stats, dx, rows, pairs, splits, st)
-         : a.dh == 32 ? bwd_of<32>(a, x, y, g, stats, dx, rows, pairs, splits, st)
-         : a.dh == 64 ? bwd_of<64>(a, x, y, g, stats, dx, rows, pairs, splits, st)
-                      : bwd_of<128>(a, x, y, g, stats, dx, rows, pairs, splits, st);
+template <typename T>
+int rel_mfma_bwd(const RelArgs& a, const T* qkv, const T* o, const T* d_o, const float* stats, T* dqkv, float* rows, float* pairs, int splits, hipStream_t st) {
+  switch (a.dh) {
+    case 16: return bwd_of<T, 16>(a, qkv, o, d_o, stats, dqkv, rows, pairs, splits, st);
+    case 32: return bwd_of<T, 32>(a, qkv, o, d_o, stats, dqkv, rows, pairs, splits, st);
+    case 64: return bwd_of<T, 64>(a, qkv, o, d_o, stats, dqkv, rows, pairs, splits, st);
+    default: return bwd_of<T, 128>(a, qkv, o, d_o, stats, dqkv, rows, pairs, splits, st);
+  }
 }
