@@ -47,25 +47,25 @@ static inline bool rel_aligned(const void* p, size_t a) { return ((size_t)p & (a
 //   by_query  a lane a query (column), its registers keys    u16 [NT][NT][64][16]
 //   by_key    a lane a key, its registers queries, block (u / 32, t / 32)
 // An entry is 4 x bucket, the byte offset into a head's table in LDS; 4 x buckets for masked pairs and for padding, where that table holds -infinity.
-//   start     int [buckets + 1]: where a bucket's pairs begin in
-//   list      int [T * T]: places of its pairs in a head's sums of dx (rel_sum_place), in the order of (t, u)
+// What reduces dx of the pairs, summed over images, to buckets.  These sums lie in blocks as in by_key, in a block registers in fours [4][64 lanes][4].
+//   order     u16 [NT][NT][64][16]: a block's pairs sorted by bucket (masked ones last), sixteen to a lane: their bytes in the block
+//   ends      u32 [NT][NT][64]: low half: which of a lane's sixteen end a run of one bucket; high half: runs of the lanes before
+//             (a lane's runs go to the block's own place, one behind the other)
+//   start     int [buckets + 1]: where a bucket's runs begin in
+//   list      int [T * T at most]: places of its runs, in the order of the blocks
 constexpr int kRelMaxT = 8192, kRelMaxBuckets = 16382;
-struct RelPlan { size_t by_query, by_key, start, list, bytes; };
+struct RelPlan { size_t by_query, by_key, order, ends, start, list, bytes; };
 static inline RelPlan rel_plan_layout(int T, int buckets) {
-  const size_t NT = (T + 31) / 32, map = align_up(NT * NT * 2048, 256);
+  const size_t NT = (T + 31) / 32, map = NT * NT * 2048;
   RelPlan p;
   p.by_query = 0;
   p.by_key = map;
-  p.start = 2 * map;
+  p.order = 2 * map;
+  p.ends = 3 * map;
+  p.start = p.ends + NT * NT * 256;
   p.list = p.start + align_up((size_t)(buckets + 1) * 4, 256);
   p.bytes = p.list + align_up((size_t)T * T * 4, 256);
   return p;
 }
 // place of row r, column c of a block in its 1024 entries
 __host__ __device__ __forceinline__ int rel_place(int r, int c) { return (((r >> 2 & 1) << 5 | c) << 4) | (r >> 3) << 2 | (r & 3); }
-// place of a pair in the sums of dx over images: blocks as in by_key, in a block registers in fours [4][64 lanes][4], which a wavefront loads and
-// stores 1 KB at a time
-__host__ __device__ __forceinline__ int rel_sum_place(int NT, int t, int u) {
-  const int r = t & 31;
-  return ((u >> 5) * NT + (t >> 5)) * 1024 + (r >> 3) * 256 + ((r >> 2 & 1) << 5 | (u & 31)) * 4 + (r & 3);
-}

@@ -8,7 +8,8 @@ struct RelArgs {
   unsigned site;
   RelDrop dr;
   const float* table;
-  const unsigned short *by_query, *by_key;
+  const unsigned short *by_query, *by_key, *order;
+  const unsigned* ends;
   const int *start, *list, *lens;
   const unsigned long long* rng;
 };

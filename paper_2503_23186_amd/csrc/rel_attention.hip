@@ -3,19 +3,52 @@
 #include "rel_attention.h"
 
 namespace {
-// the splits' sums of the pairs into the first's place
-__global__ void __launch_bounds__(256) rel_splits_kernel(float4* pairs, size_t n, int splits) {
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= n) return;
-  float4 s = pairs[i];
-  for (int k = 1; k < splits; ++k) {
-    const float4 v = pairs[k * n + i];
-    s.x += v.x, s.y += v.y, s.z += v.z, s.w += v.w;
+// Sums of a block's pairs over the splits, then of its runs of one bucket.  A wavefront to a block and `heads_of` heads; the block's sums go through LDS in the
+// plan's order, sixteen to a lane, and a lane's runs to the block's place in the first split.  A grid's map leaves 100 to 200 runs of 1024 pairs, so that the
+// gather behind this moves that much less (4096 tokens, 12 heads: 695 us for a gather of all pairs).
+__global__ void __launch_bounds__(256) rel_runs_kernel(RelArgs a, float* pairs, int splits, int heads_of) {
+  __shared__ __align__(16) float sm[4][1024];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, blocks = a.NT * a.NT, block = blockIdx.x * 4 + wave;
+  if (block >= blocks) return;
+  float* mine = sm[wave];
+  const uint4* op = reinterpret_cast<const uint4*>(a.order + (size_t)block * 1024 + lane * 16);
+  const uint4 o0 = op[0], o1 = op[1];
+  const unsigned w[8] = {o0.x, o0.y, o0.z, o0.w, o1.x, o1.y, o1.z, o1.w}, ends = a.ends[(size_t)block * 64 + lane];
+  const int h1 = min(a.heads, ((int)blockIdx.y + 1) * heads_of);
+  for (int h = blockIdx.y * heads_of; h < h1; ++h) {
+    float* m = pairs + ((size_t)h * blocks + block) * 1024;
+    float4 s[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) s[k] = *reinterpret_cast<const float4*>(m + k * 256 + lane * 4);
+    for (int x = 1; x < splits; ++x) {
+      const float* n = m + (size_t)x * a.heads * blocks * 1024;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float4 v = *reinterpret_cast<const float4*>(n + k * 256 + lane * 4);
+        s[k].x += v.x, s[k].y += v.y, s[k].z += v.z, s[k].w += v.w;
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) *reinterpret_cast<float4*>(mine + k * 256 + lane * 4) = s[k];
+    __builtin_amdgcn_wave_barrier();      // the wavefront's own part of LDS, which it uses in order
+    float v[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = *reinterpret_cast<const float*>(reinterpret_cast<const char*>(mine) + (e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xffffu));
+    __builtin_amdgcn_wave_barrier();
+    float* out = m + (ends >> 16);
+    float run = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      run += v[e];
+      if (ends >> e & 1) {
+        *out++ = run;
+        run = 0.f;
+      }
+    }
   }
-  pairs[i] = s;
 }
 
-// `lanes` threads to a bucket and head, which take its pairs by turns; a workgroup has neighbouring buckets, whose pairs lie beside each other
+// `lanes` threads to a bucket and head, which take its runs by turns; a workgroup has neighbouring buckets, whose runs lie beside each other
 // in maps by distance.
 __global__ void __launch_bounds__(256) rel_buckets_kernel(RelArgs a, const float* __restrict__ pairs, int lanes, float* __restrict__ dtable) {
   __shared__ float sm[256];
@@ -68,7 +101,8 @@ RelArgs args_of(const cnnk_rel_desc* d, RelDrop dr, const float* table, const vo
   a.site = d->site;
   a.dr = dr;
   a.table = table;
-  a.by_query = a.by_key = nullptr;
+  a.by_query = a.by_key = a.order = nullptr;
+  a.ends = nullptr;
   a.start = a.list = nullptr;
   a.lens = lens;
   a.rng = rng;
@@ -76,6 +110,8 @@ RelArgs args_of(const cnnk_rel_desc* d, RelDrop dr, const float* table, const vo
     const RelPlan at = rel_plan_layout(d->T, d->buckets);
     a.by_query = (const unsigned short*)((const char*)plan + at.by_query);
     a.by_key = (const unsigned short*)((const char*)plan + at.by_key);
+    a.order = (const unsigned short*)((const char*)plan + at.order);
+    a.ends = (const unsigned*)((const char*)plan + at.ends);
     a.start = (const int*)((const char*)plan + at.start);
     a.list = (const int*)((const char*)plan + at.list);
   }
@@ -133,10 +169,8 @@ extern "C" int cnnk_rel_attention_bwd(const cnnk_rel_desc* d, const void* qkv, c
                     ? rel_mfma_bwd(a, (const bf16_t*)qkv, (const bf16_t*)o, (const bf16_t*)d_o, stats, (bf16_t*)dqkv, rows, pairs, splits, st)
                     : rel_mfma_bwd(a, (const float*)qkv, (const float*)o, (const float*)d_o, stats, (float*)dqkv, rows, pairs, splits, st);
   if (r != CNNK_OK || !pairs) return r;
-  if (splits > 1) {
-    const size_t n = (size_t)d->heads * a.NT * a.NT * 256;
-    rel_splits_kernel<<<(unsigned)((n + 255) / 256), 256, 0, st>>>((float4*)pairs, n, splits);
-  }
+  const int blocks = a.NT * a.NT, heads_of = (int)((long)blocks * d->heads >= 65536 ? 4 : 1);
+  rel_runs_kernel<<<dim3((blocks + 3) / 4, (d->heads + heads_of - 1) / heads_of), 256, 0, st>>>(a, pairs, splits, heads_of);
   // enough threads to fill the device where buckets are few
   int lanes = 8;
   while (lanes < 256 && (long)d->buckets * d->heads * lanes < 131072) lanes *= 2;

@@ -1,9 +1,10 @@
-// Bucket maps and their plans (rel.h has the layout).  A plan is made once for a map, so these kernels are plain: a counting sort of the pairs
-// by bucket in parts of the map, stable, so that a bucket's sum has one order.
+// Bucket maps and their plans (rel.h has the layout).  A plan is made once for a map, so these kernels are plain: a sort of each block's pairs by
+// bucket, then a counting sort of all blocks' runs, stable, so that a bucket's sum has one order.
 #include "rel.h"
 
 namespace {
-constexpr int kParts = 256;      // of the T * T pairs
+constexpr int kParts = 256;              // of the places of runs
+constexpr unsigned short kNoRun = 0xffff;
 
 __global__ void __launch_bounds__(256) buckets_grid_kernel(int gw, int gh, int cls, int T, int* __restrict__ bucket) {
   const int n = (2 * gh - 1) * (2 * gw - 1);
@@ -31,15 +32,61 @@ __global__ void __launch_bounds__(256) plan_maps_kernel(int T, int NT, int bucke
   }
 }
 
-// pairs of each bucket in each part
-__global__ void __launch_bounds__(256) plan_count_kernel(int pairs, int per, int buckets, const int* __restrict__ bucket, int* __restrict__ count) {
+// A workgroup to a block of 32 keys x 32 queries: its pairs sorted by bucket and place (bitonic), runs within sixteen of them, each run's bucket.
+__global__ void __launch_bounds__(256) plan_order_kernel(int T, int NT, int buckets, const int* __restrict__ bucket, unsigned short* __restrict__ order,
+                                                         unsigned* __restrict__ ends, unsigned short* __restrict__ run_bucket) {
+  __shared__ unsigned key[1024];
+  __shared__ unsigned before[64];
+  const int block = blockIdx.x, u0 = block / NT * 32, t0 = block % NT * 32;
+  for (int i = threadIdx.x; i < 1024; i += 256) {
+    const int lane = i >> 2 & 63, reg = (i >> 8) * 4 + (i & 3), t = t0 + (reg >> 2) * 8 + (lane >> 5) * 4 + (reg & 3), u = u0 + (lane & 31);
+    int k = buckets;
+    if (t < T && u < T) {
+      k = bucket[(size_t)t * T + u];
+      if (k < 0 || k >= buckets) k = buckets;
+    }
+    key[i] = (unsigned)k << 10 | i;
+    run_bucket[(size_t)block * 1024 + i] = kNoRun;
+  }
+  for (int size = 2; size <= 1024; size *= 2)
+    for (int step = size / 2; step > 0; step /= 2) {
+      __syncthreads();
+      for (int p = threadIdx.x; p < 512; p += 256) {
+        const int i = (p / step) * 2 * step + p % step, j = i + step;
+        const unsigned a = key[i], b = key[j];
+        if ((a > b) == ((i & size) == 0)) key[i] = b, key[j] = a;
+      }
+    }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 1024; i += 256) order[(size_t)block * 1024 + i] = (unsigned short)((key[i] & 1023u) * 4);
+  unsigned flags = 0;
+  if (threadIdx.x < 64) {
+    for (int e = 0; e < 16; ++e) {
+      const int i = threadIdx.x * 16 + e;
+      const unsigned k = key[i] >> 10;
+      if (k < (unsigned)buckets && (e == 15 || key[i + 1] >> 10 != k)) flags |= 1u << e;
+    }
+    before[threadIdx.x] = __popc(flags);
+  }
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    unsigned at = 0;
+    for (int l = 0; l < (int)threadIdx.x; ++l) at += before[l];
+    ends[(size_t)block * 64 + threadIdx.x] = flags | at << 16;
+    for (int e = 0; e < 16; ++e)
+      if (flags >> e & 1) run_bucket[(size_t)block * 1024 + at++] = (unsigned short)(key[threadIdx.x * 16 + e] >> 10);
+  }
+}
+
+// runs of each bucket in each part
+__global__ void __launch_bounds__(256) plan_count_kernel(int places, int per, int buckets, const unsigned short* __restrict__ run_bucket, int* __restrict__ count) {
   extern __shared__ int cnt[];
   for (int k = threadIdx.x; k < buckets; k += 256) cnt[k] = 0;
   __syncthreads();
-  const int end = min(pairs, ((int)blockIdx.x + 1) * per);
+  const int end = min(places, ((int)blockIdx.x + 1) * per);
   for (int i = blockIdx.x * per + threadIdx.x; i < end; i += 256) {
-    const int k = bucket[i];
-    if (k >= 0 && k < buckets) atomicAdd(cnt + k, 1);
+    const int k = run_bucket[i];
+    if (k < buckets) atomicAdd(cnt + k, 1);
   }
   __syncthreads();
   for (int k = threadIdx.x; k < buckets; k += 256) count[(size_t)blockIdx.x * buckets + k] = cnt[k];
@@ -75,18 +122,19 @@ __global__ void __launch_bounds__(1024) plan_starts_kernel(int buckets, int* __r
   if (k0 < buckets && k1 == buckets) start[buckets] = at;
 }
 
-// one wavefront to a part, 64 pairs at a time; among them a pair comes behind those before it in the same bucket
-__global__ void __launch_bounds__(64) plan_list_kernel(int T, int NT, int pairs, int per, int buckets, const int* __restrict__ bucket, const int* __restrict__ count,
+// one wavefront to a part, 64 places at a time; among them a run comes behind those before it in the same bucket
+__global__ void __launch_bounds__(64) plan_list_kernel(int places, int per, int buckets, const unsigned short* __restrict__ run_bucket, const int* __restrict__ count,
                                                        const int* __restrict__ start, int* __restrict__ list) {
   extern __shared__ int at[];
   const int lane = threadIdx.x;
   for (int k = lane; k < buckets; k += 64) at[k] = start[k] + count[(size_t)blockIdx.x * buckets + k];
   __syncthreads();
-  const int end = min(pairs, ((int)blockIdx.x + 1) * per);
+  const int end = min(places, ((int)blockIdx.x + 1) * per);
   for (int i0 = blockIdx.x * per; i0 < end; i0 += 64) {
     const int i = i0 + lane;
-    int k = i < end ? bucket[i] : -1;
-    if (k < 0 || k >= buckets) k = -1;
+    int k = i < end ? run_bucket[i] : kNoRun;
+    if (k >= buckets) k = -1;
+    if (!__any(k >= 0)) continue;
     int before = 0, all = 0;
     for (int j = 0; j < 64; ++j) {
       const int same = __builtin_amdgcn_readlane(k, j) == k;
@@ -96,14 +144,17 @@ __global__ void __launch_bounds__(64) plan_list_kernel(int T, int NT, int pairs,
     const int place = k >= 0 ? at[k] + before : 0;
     __syncthreads();
     if (k >= 0) {
-      const int t = i / T, u = i - t * T;
-      list[place] = rel_sum_place(NT, t, u);
+      list[place] = i;
       if (before == all - 1) at[k] = place + 1;
     }
     __syncthreads();
   }
 }
 
+size_t runs_bytes(int T) {
+  const size_t NT = (T + 31) / 32;
+  return NT * NT * 2048;
+}
 bool supported(int T, int buckets) { return T <= kRelMaxT && buckets <= kRelMaxBuckets; }
 }  // namespace
 
@@ -122,7 +173,7 @@ extern "C" size_t cnnk_rel_plan_bytes(int T, int buckets) {
   return T > 0 && buckets > 0 && supported(T, buckets) ? rel_plan_layout(T, buckets).bytes : 0;
 }
 extern "C" size_t cnnk_rel_plan_workspace_bytes(int T, int buckets) {
-  return T > 0 && buckets > 0 && supported(T, buckets) ? align_up((size_t)kParts * buckets * 4, 256) : 0;
+  return T > 0 && buckets > 0 && supported(T, buckets) ? runs_bytes(T) + align_up((size_t)kParts * buckets * 4, 256) : 0;
 }
 
 extern "C" int cnnk_rel_plan(int T, int buckets, const int* bucket, void* plan, void* ws, size_t ws_bytes, void* stream) {
@@ -134,13 +185,15 @@ extern "C" int cnnk_rel_plan(int T, int buckets, const int* bucket, void* plan, 
   hipStream_t st = (hipStream_t)stream;
   const RelPlan at = rel_plan_layout(T, buckets);
   char* p = (char*)plan;
-  int *count = (int*)ws, *start = (int*)(p + at.start), *list = (int*)(p + at.list);
-  const int NT = (T + 31) / 32, pairs = T * T, per = ((pairs + kParts - 1) / kParts + 63) / 64 * 64;
-  const size_t lds = (size_t)buckets * 4, blocks = ((size_t)NT * NT * 1024 + 255) / 256;
+  unsigned short* runs = (unsigned short*)ws;
+  int *count = (int*)((char*)ws + runs_bytes(T)), *start = (int*)(p + at.start), *list = (int*)(p + at.list);
+  const int NT = (T + 31) / 32, places = NT * NT * 1024, per = ((places + kParts - 1) / kParts + 63) / 64 * 64;
+  const size_t lds = (size_t)buckets * 4, blocks = ((size_t)places + 255) / 256;
   plan_maps_kernel<<<(unsigned)(blocks < 16384 ? blocks : 16384), 256, 0, st>>>(T, NT, buckets, bucket, (unsigned short*)(p + at.by_query), (unsigned short*)(p + at.by_key));
-  plan_count_kernel<<<kParts, 256, lds, st>>>(pairs, per, buckets, bucket, count);
+  plan_order_kernel<<<NT * NT, 256, 0, st>>>(T, NT, buckets, bucket, (unsigned short*)(p + at.order), (unsigned*)(p + at.ends), runs);
+  plan_count_kernel<<<kParts, 256, lds, st>>>(places, per, buckets, runs, count);
   plan_parts_kernel<<<(buckets + 255) / 256, 256, 0, st>>>(buckets, count, start);
   plan_starts_kernel<<<1, 1024, 0, st>>>(buckets, start);
-  plan_list_kernel<<<kParts, 64, lds, st>>>(T, NT, pairs, per, buckets, bucket, count, start, list);
+  plan_list_kernel<<<kParts, 64, lds, st>>>(places, per, buckets, runs, count, start, list);
   return launch_status();
 }

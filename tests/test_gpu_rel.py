@@ -147,20 +147,40 @@ def test_plans_are_reproducible_and_ignore_what_they_overwrite(K):
     for p, fill in ((a, 255), (b, 0)):
         ws = torch.full((K.cnnk_rel_plan_workspace_bytes(T, n),), fill, dtype=torch.uint8, device=DEV)
         K.cnnk_rel_plan(T, n, m, p, ws, ws.numel())
-    NT = (T + 31) // 32
-    maps = 2 * NT * NT * 2048                                    # then the starts and the lists
-    start = a[maps:maps + 4 * (n + 1)].view(torch.int32).cpu().numpy()
-    ids = m.cpu().numpy().ravel()
-    want = np.concatenate([[0], np.cumsum([(ids == k).sum() for k in range(n)])])
-    assert (start == want).all()
-    at = maps + (4 * (n + 1) + 255) // 256 * 256
-    lists = [x[at:at + 4 * int(start[-1])].view(torch.int32) for x in (a, b)]
-    assert torch.equal(lists[0], lists[1]) and torch.equal(a[:maps], b[:maps])
-    order = lists[0].cpu().numpy()
-    block, place = order >> 10, order & 1023                     # blocks of keys, in them of queries; [4][64 lanes][4] of a block
-    lane, reg = place >> 2 & 63, (place >> 8) * 4 + (place & 3)
-    t, u = block % NT * 32 + (reg >> 2) * 8 + (lane >> 5) * 4 + (reg & 3), block // NT * 32 + (lane & 31)
-    assert (t * T + u == np.concatenate([np.flatnonzero(ids == k) for k in range(n)])).all()
+    NT, ids = (T + 31) // 32, m.cpu().numpy()
+    ids = np.where((ids >= 0) & (ids < n), ids, n)
+    padded = np.full((NT * 32, NT * 32), n)
+    padded[:T, :T] = ids
+    part = lambda x, at, count, dt: x[at:at + count * np.dtype(dt).itemsize].cpu().numpy().view(dt)
+    size = NT * NT * 1024
+    # the two maps: lane (r // 4 % 2) * 32 + c, register r // 8 * 4 + r % 4 of row r, column c of a block; a lane is a query, then a key
+    r, c = np.arange(32)[:, None], np.arange(32)[None, :]
+    place = ((r // 4 % 2) * 32 + c) * 16 + r // 8 * 4 + r % 4
+    for k, look in enumerate((lambda i, j: padded[i * 32:i * 32 + 32, j * 32:j * 32 + 32].T, lambda i, j: padded[j * 32:j * 32 + 32, i * 32:i * 32 + 32])):
+        got = part(a, k * size * 2, size, np.uint16).reshape(NT, NT, 1024)
+        for i in range(NT):
+            for j in range(NT):
+                assert (got[i, j][place] == 4 * look(i, j)).all()
+    # every pair of a bucket is in just one run, every run in the list of its bucket, in the order of the blocks
+    order = part(a, 2 * size * 2, size, np.uint16).reshape(NT * NT, 64, 16) // 4
+    ends = part(a, 3 * size * 2, NT * NT * 64, np.uint32).reshape(NT * NT, 64)
+    start = part(a, 3 * size * 2 + NT * NT * 256, n + 1, np.int32)
+    at = 3 * size * 2 + NT * NT * 256 + (4 * (n + 1) + 255) // 256 * 256
+    lists = [part(x, at, int(start[-1]), np.int32) for x in (a, b)]
+    assert (lists[0] == lists[1]).all() and torch.equal(a[:3 * size * 2], b[:3 * size * 2])
+    where = np.full(size, -1)                                    # bucket of the run at a place
+    for x in range(NT * NT):
+        assert (np.sort(order[x].ravel()) == np.arange(1024)).all()
+        lane, reg = order[x] >> 2 & 63, (order[x] >> 8) * 4 + (order[x] & 3)
+        t, u = x % NT * 32 + (reg >> 2) * 8 + (lane >> 5) * 4 + (reg & 3), x // NT * 32 + (lane & 31)
+        k = padded[t, u]
+        flags = ends[x][:, None] >> np.arange(16)[None, :] & 1
+        assert ((ends[x] >> 16) == np.concatenate([[0], np.cumsum(flags.sum(1))])[:64]).all()
+        last = np.concatenate([k[:, 1:] != k[:, :-1], np.ones((64, 1), bool)], 1) & (k < n)
+        assert (flags == last).all() and (np.diff(k.ravel()) >= 0).all()
+        where[x * 1024:x * 1024 + flags.sum()] = k[flags == 1]
+    assert (lists[0] == np.concatenate([np.flatnonzero(where == k) for k in range(n)])).all()
+    assert (start == np.concatenate([[0], np.cumsum([(where == k).sum() for k in range(n)])])).all()
 
 
 # ---- attention ---------------------------------------------------------------------------------------------------------------
