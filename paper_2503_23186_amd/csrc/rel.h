@@ -6,15 +6,16 @@
 // ---- generator -----------------------------------------------------------------------------------------------
 // Philox4x32 with seven rounds (J. Salmon, M. Moraes, R. Dror, D. Shaw, SC 2011), the fewest with which its authors found no
 // failing test.  A round is two 32 x 32 -> 64-bit products (v_mad_u64_u32).
+__device__ __forceinline__ unsigned xor3(unsigned a, unsigned b, unsigned c) { return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96); }
 struct RelWords { unsigned w[4]; };
 struct RelKey { unsigned k0, k1; };
 __device__ __forceinline__ RelWords rel_words(unsigned c0, unsigned c1, unsigned c2, unsigned c3, RelKey k) {
 #pragma unroll
   for (int i = 0; i < 7; ++i) {
     const unsigned long long a = (unsigned long long)c0 * 0xD2511F53u, b = (unsigned long long)c2 * 0xCD9E8D57u;
-    c0 = (unsigned)(b >> 32) ^ c1 ^ k.k0;
+    c0 = xor3((unsigned)(b >> 32), c1, k.k0);
     c1 = (unsigned)b;
-    c2 = (unsigned)(a >> 32) ^ c3 ^ k.k1;
+    c2 = xor3((unsigned)(a >> 32), c3, k.k1);
     c3 = (unsigned)a;
     k.k0 += 0x9E3779B9u;
     k.k1 += 0xBB67AE85u;

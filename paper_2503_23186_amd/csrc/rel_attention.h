@@ -20,7 +20,13 @@ __device__ __forceinline__ int rel_tokens(const RelArgs& a, int b) {
   return n < 0 ? 0 : n > a.T ? a.T : n;
 }
 
-// rows: [B * heads][3][Tp] floats; pairs (NULL: no gradient of the table): [splits][heads][NT][NT][1024].  T: bf16_t or float
+// the first workgroup that has images of a head, and how many have them
+__host__ __device__ __forceinline__ int rel_first_group(int head, int B, int units) { return (int)((long long)head * B / units); }
+__host__ __device__ __forceinline__ int rel_groups(int head, int B, int units) {
+  return (int)(((long long)head * B + B - 1) / units) - rel_first_group(head, B, units) + 1;
+}
+// rows: [B * heads][3][Tp] floats; pairs (NULL: no gradient of the table): [slots][heads][NT][NT][1024]; units: (head, image) pairs
+// that a workgroup of the walk for dk and dv has.  T: bf16_t or float
 template <typename T> int rel_mfma_fwd(const RelArgs& a, const T* qkv, T* o, float* stats, hipStream_t st);
 template <typename T>
-int rel_mfma_bwd(const RelArgs& a, const T* qkv, const T* o, const T* d_o, const float* stats, T* dqkv, float* rows, float* pairs, int splits, hipStream_t st);
+int rel_mfma_bwd(const RelArgs& a, const T* qkv, const T* o, const T* d_o, const float* stats, T* dqkv, float* rows, float* pairs, int units, hipStream_t st);

@@ -3,10 +3,10 @@
 #include "rel_attention.h"
 
 namespace {
-// Sums of a block's pairs over the splits, then of its runs of one bucket.  A wavefront to a block and `heads_of` heads; the block's sums go through LDS in the
-// plan's order, sixteen to a lane, and a lane's runs to the block's place in the first split.  A grid's map leaves 100 to 200 runs of 1024 pairs, so that the
+// Sums of a block's pairs over the workgroups' slots, then of its runs of one bucket.  A wavefront to a block and `heads_of` heads; the block's sums go through LDS in the
+// plan's order, sixteen to a lane, and a lane's runs to the block's place in the first slot.  A grid's map leaves 100 to 200 runs of 1024 pairs, so that the
 // gather behind this moves that much less (4096 tokens, 12 heads: 695 us for a gather of all pairs).
-__global__ void __launch_bounds__(256) rel_runs_kernel(RelArgs a, float* pairs, int splits, int heads_of) {
+__global__ void __launch_bounds__(256) rel_runs_kernel(RelArgs a, float* pairs, int units, int heads_of) {
   __shared__ __align__(16) float sm[4][1024];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, blocks = a.NT * a.NT, block = blockIdx.x * 4 + wave;
   if (block >= blocks) return;
@@ -20,7 +20,8 @@ __global__ void __launch_bounds__(256) rel_runs_kernel(RelArgs a, float* pairs, 
     float4 s[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) s[k] = *reinterpret_cast<const float4*>(m + k * 256 + lane * 4);
-    for (int x = 1; x < splits; ++x) {
+    const int slots = rel_groups(h, a.B, units);
+    for (int x = 1; x < slots; ++x) {
       const float* n = m + (size_t)x * a.heads * blocks * 1024;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -117,15 +118,19 @@ RelArgs args_of(const cnnk_rel_desc* d, RelDrop dr, const float* table, const vo
   }
   return a;
 }
-// scratch of the backward pass: three floats for each row, and the sums of every pair, `splits` times over
+// scratch of the backward pass: three floats for each row, and the sums of every pair, as often as a head's images lie in different workgroups
 size_t rows_bytes(const cnnk_rel_desc* d) { return align_up((size_t)d->B * d->heads * 3 * ((d->T + 63) / 64 * 64) * 4, 256); }
-int splits_of(const cnnk_rel_desc* d) {
-  const long NT = (d->T + 31) / 32, groups = d->heads * ((NT + 3) / 4), want = (512 + groups - 1) / groups;
-  return (int)(want < d->B ? want : d->B);
+// (head, image) pairs to a workgroup of the walk for dk and dv: as many as give every workgroup that the device holds (two to a CU, or one with heads of 128 or a
+// large table) the same number, so that there is one round of them and few sums to add up.
+int units_of(const cnnk_rel_desc* d) {
+  const long NT = (d->T + 31) / 32, held = d->dh == 128 || d->buckets > 10000 ? 256 : 512;
+  const long units = ((long)d->B * d->heads * ((NT + 3) / 4) + held - 1) / held;
+  return (int)(units < d->B ? units : d->B);
 }
 size_t pairs_bytes(const cnnk_rel_desc* d) {
   const size_t NT = (d->T + 31) / 32;
-  return (size_t)splits_of(d) * d->heads * NT * NT * 4096;
+  const int units = units_of(d);
+  return (size_t)((d->B + units - 2) / units + 1) * d->heads * NT * NT * 4096;
 }
 
 }  // namespace
@@ -164,13 +169,13 @@ extern "C" int cnnk_rel_attention_bwd(const cnnk_rel_desc* d, const void* qkv, c
   const RelArgs a = args_of(d, dr, table, plan, lens, rng);
   float *rows = (float*)ws, *pairs = d->buckets && dtable ? (float*)((char*)ws + rows_bytes(d)) : nullptr;
   hipStream_t st = (hipStream_t)stream;
-  const int splits = splits_of(d);
+  const int units = units_of(d);
   const int r = d->dtype == CNNK_BF16
-                    ? rel_mfma_bwd(a, (const bf16_t*)qkv, (const bf16_t*)o, (const bf16_t*)d_o, stats, (bf16_t*)dqkv, rows, pairs, splits, st)
-                    : rel_mfma_bwd(a, (const float*)qkv, (const float*)o, (const float*)d_o, stats, (float*)dqkv, rows, pairs, splits, st);
+                    ? rel_mfma_bwd(a, (const bf16_t*)qkv, (const bf16_t*)o, (const bf16_t*)d_o, stats, (bf16_t*)dqkv, rows, pairs, units, st)
+                    : rel_mfma_bwd(a, (const float*)qkv, (const float*)o, (const float*)d_o, stats, (float*)dqkv, rows, pairs, units, st);
   if (r != CNNK_OK || !pairs) return r;
   const int blocks = a.NT * a.NT, heads_of = (int)((long)blocks * d->heads >= 65536 ? 4 : 1);
-  rel_runs_kernel<<<dim3((blocks + 3) / 4, (d->heads + heads_of - 1) / heads_of), 256, 0, st>>>(a, pairs, splits, heads_of);
+  rel_runs_kernel<<<dim3((blocks + 3) / 4, (d->heads + heads_of - 1) / heads_of), 256, 0, st>>>(a, pairs, units, heads_of);
   // enough threads to fill the device where buckets are few
   int lanes = 8;
   while (lanes < 256 && (long)d->buckets * d->heads * lanes < 131072) lanes *= 2;

@@ -267,11 +267,13 @@ __device__ __forceinline__ float both_halves_sum(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
+// Keeps the compiler from turning a branch that one tile of a walk takes into selects in every tile (a tenth of the forward pass).
+__device__ __forceinline__ void only_here() { asm volatile(""); }
 __device__ __forceinline__ int key_of(int i, int h) { return (i >> 2) * 8 + h * 4 + (i & 3); }
 
 // ---- forward ---------------------------------------------------------------------------------------------------------------
 template <typename T, int DH, bool BIAS, bool DROP>
-__global__ void __launch_bounds__(512, sizeof(T) == 2 && DH <= 64 ? 3 : 2) rel_mfma_fwd_kernel(RelArgs a, const T* __restrict__ qkv, T* __restrict__ o,
+__global__ void __launch_bounds__(512, sizeof(T) == 2 && DH <= 64 ? 4 : 2) rel_mfma_fwd_kernel(RelArgs a, const T* __restrict__ qkv, T* __restrict__ o,
                                                                              float* __restrict__ stats, int parts) {
   using D = Dim<T, DH>;
   constexpr int TS = D::KB / 32, TILE = D::PLANE / TS;      // tiles of a stage, bytes of a tile's rows in a plane
@@ -320,6 +322,7 @@ __global__ void __launch_bounds__(512, sizeof(T) == 2 && DH <= 64 ? 3 : 2) rel_m
       const unsigned char *Ks = smem + (stage & 1) * D::STAGE + t % TS * TILE, *Vs = Ks + D::MAT;
       f32x16_t x = score_tile<T, DH, BIAS>(Ks, bq, table, mr, a.scale, lane);
       if (t * 32 + 32 > n) {
+        only_here();
 #pragma unroll
         for (int i = 0; i < 16; ++i)
           if (t * 32 + key_of(i, h) >= n) x[i] = -INFINITY;
@@ -452,6 +455,7 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
         dx[i] = p[i] * (DROP ? fmaf(dx[i], w, -delta) : dx[i] - delta);
       }
       if (t * 32 + 32 > n) {       // keys past the image's tokens: rows of zeros, whose probabilities may be infinite
+        only_here();
 #pragma unroll
         for (int i = 0; i < 16; ++i)
           if (t * 32 + key_of(i, h) >= n) p[i] = dx[i] = 0.f;
@@ -481,31 +485,39 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
 }
 
 // ---- backward: dk and dv, and dx of every pair summed over images ----------------------------------------------------------------
-// A workgroup has the keys of its part for a head of every `splits`-th image, one after the other.  Where the table learns, each wavefront adds dx of its keys
-// to pairs [splits][heads][NT keys][NT queries][4][64][4]: a tile's sums so far come in while its scores are formed; they are a wavefront's own, in
-// the caches, so the sum over images has one order and needs no atomics.
+// A workgroup has the keys of its part for `units` (head, image) pairs, one after the other, images before heads.  Where the table learns, each wavefront adds
+// dx of its keys to pairs [slot][heads][NT keys][NT queries][4][64][4], the slot being the workgroup's number among those that have images of the head: a
+// tile's sums so far come in while its scores are formed; they are a wavefront's own, in the caches, so the sum over images has one order and needs
+// no atomics.
 template <typename T, int DH, bool BIAS, bool DROP>
 __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mfma_dkv_kernel(RelArgs a, const T* __restrict__ qkv, const T* __restrict__ d_o,
                                                                              const float* __restrict__ rows, T* __restrict__ dqkv, float* pairs, int parts,
-                                                                             int splits) {
+                                                                             int units) {
   using D = Dim<T, DH>;
   constexpr int TS = D::KB / 32, TILE = D::PLANE / TS;      // tiles of a stage, bytes of a tile's rows in a plane
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int STAGE = D::STAGE + 3 * D::KB * 4;
-  int sh, part;
-  if (!head_part(splits * a.heads, parts, &sh, &part)) return;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = blockDim.x >> 6, h = lane >> 5;
-  const int split = sh / a.heads, head = sh - split * a.heads, d = a.heads * DH;
+  int group, part;
+  const int all = a.B * a.heads;
+  if (!head_part((all + units - 1) / units, parts, &group, &part)) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = blockDim.x >> 6, h = lane >> 5, d = a.heads * DH;
   const size_t ld = 3 * (size_t)d;
   const int u0 = (part * waves + wave) * 32, u = u0 + (lane & 31), first = part * waves * 32;
   float* table = reinterpret_cast<float*>(smem + 2 * STAGE);
-  if (BIAS) table_load(2 * STAGE, table, a, head, wave, waves, lane);
   RelKey key{0u, 0u};
   if (DROP) key = rel_key(a.rng, a.site);
   const unsigned short* map = BIAS ? a.by_key + (size_t)(u0 >> 5) * a.NT * 1024 : nullptr;
-  float* sums = BIAS && pairs ? pairs + (((size_t)split * a.heads + head) * a.NT + (u0 >> 5)) * a.NT * 1024 + lane * 4 : nullptr;
-  for (int b = split; b < a.B; b += splits) {
+  const int end = min(all, (group + 1) * units);
+  int head = group * units / a.B, b = group * units - head * a.B;
+  bool fresh = true;                 // the first image of its head here
+  for (int unit = group * units; unit < end; ++unit, ++b) {
+    if (b == a.B) b = 0, ++head, fresh = true;
+    const bool first_image = fresh;
+    fresh = false;
     const int n = rel_tokens(a, b), bh = b * a.heads + head;
+    if (unit != group * units) workgroup_barrier();       // the image before is read
+    if (BIAS && first_image) table_load(2 * STAGE, table, a, head, wave, waves, lane);
+    float* sums = BIAS && pairs ? pairs + (((size_t)(group - rel_first_group(head, a.B, units)) * a.heads + head) * a.NT + (u0 >> 5)) * a.NT * 1024 + lane * 4 : nullptr;
     const T* base = qkv + (size_t)b * a.T * ld + head * DH;
     const int tiles = first < n ? (n + 31) >> 5 : 0;
     const bool mine = u0 < n;
@@ -513,7 +525,6 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
 #pragma unroll
     for (int mt = 0; mt < D::NM; ++mt) dk[mt] = dv[mt] = zero16();
     if (tiles) {
-      if (b != split) workgroup_barrier();       // the image before is read
       Stager<T, DH> st;
       st.init(base, d_o + (size_t)b * a.T * d + head * DH, (unsigned)(ld * sizeof(T)), (unsigned)(d * sizeof(T)), n, lane);
       const i32x4_t rs = make_desc(rows + (size_t)bh * 3 * a.Tp, (unsigned)a.Tp * 12u);
@@ -550,7 +561,7 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
         if (BIAS && sums) {
 #pragma unroll
           for (int k = 0; k < 4; ++k) was[k] = float4{0.f, 0.f, 0.f, 0.f};
-          if (b != split) {
+          if (!first_image) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) was[k] = *reinterpret_cast<const float4*>(sums + (size_t)t * 1024 + k * 256);
           }
@@ -583,6 +594,7 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
         }
         if (BIAS && sums) {
           if (u0 + 32 > n) {       // keys past the image's tokens: probabilities that may be infinite
+            only_here();
 #pragma unroll
             for (int i = 0; i < 16; ++i) dx[i] = u < n ? dx[i] : 0.f;
           }
@@ -596,7 +608,7 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
       }
     }
     if (u0 >= a.T) continue;
-    if (BIAS && sums && b == split) {      // blocks that this image has no pairs in
+    if (BIAS && sums && first_image) {      // blocks that this image has no pairs in
       for (int t = mine ? tiles : 0; t < a.NT; ++t)
 #pragma unroll
         for (int k = 0; k < 4; ++k) *reinterpret_cast<float4*>(sums + (size_t)t * 1024 + k * 256) = float4{0.f, 0.f, 0.f, 0.f};
@@ -636,14 +648,14 @@ int fwd_launch(const RelArgs& a, const T* qkv, T* o, float* stats, hipStream_t s
   return launch_status();
 }
 template <typename T, int DH, bool BIAS, bool DROP>
-int bwd_launch(const RelArgs& a, const T* qkv, const T* o, const T* d_o, const float* stats, T* dqkv, float* rows, float* pairs, int splits, hipStream_t st) {
+int bwd_launch(const RelArgs& a, const T* qkv, const T* o, const T* d_o, const float* stats, T* dqkv, float* rows, float* pairs, int units, hipStream_t st) {
   const size_t lds = 2 * Dim<T, DH>::STAGE + table_bytes(a), lds_kv = lds + 2 * 3 * Dim<T, DH>::KB * 4;
   const int waves = waves_of(a, lds_kv, DH <= 64), parts = (a.NT + waves - 1) / waves, heads = a.B * a.heads;
   const auto dq = rel_mfma_dq_kernel<T, DH, BIAS, DROP>;
   const auto dkv = rel_mfma_dkv_kernel<T, DH, BIAS, DROP>;
   if (allow_lds(dq, lds) != CNNK_OK || allow_lds(dkv, lds_kv) != CNNK_OK) return CNNK_ERR_HIP;
   dq<<<(heads + 7) / 8 * 8 * parts, 64 * waves, lds, st>>>(a, qkv, o, d_o, stats, dqkv, rows, parts);
-  dkv<<<(splits * a.heads + 7) / 8 * 8 * parts, 64 * waves, lds_kv, st>>>(a, qkv, d_o, rows, dqkv, pairs, parts, splits);
+  dkv<<<((heads + units - 1) / units + 7) / 8 * 8 * parts, 64 * waves, lds_kv, st>>>(a, qkv, d_o, rows, dqkv, pairs, parts, units);
   return launch_status();
 }
 template <typename T, int DH> int fwd_of(const RelArgs& a, const T* qkv, T* o, float* stats, hipStream_t st) {
@@ -651,12 +663,12 @@ template <typename T, int DH> int fwd_of(const RelArgs& a, const T* qkv, T* o, f
   return a.dr.q ? fwd_launch<T, DH, false, true>(a, qkv, o, stats, st) : fwd_launch<T, DH, false, false>(a, qkv, o, stats, st);
 }
 template <typename T, int DH>
-int bwd_of(const RelArgs& a, const T* qkv, const T* o, const T* d_o, const float* stats, T* dqkv, float* rows, float* pairs, int splits, hipStream_t st) {
+int bwd_of(const RelArgs& a, const T* qkv, const T* o, const T* d_o, const float* stats, T* dqkv, float* rows, float* pairs, int units, hipStream_t st) {
   if (a.buckets)
-    return a.dr.q ? bwd_launch<T, DH, true, true>(a, qkv, o, d_o, stats, dqkv, rows, pairs, splits, st)
-                  : bwd_launch<T, DH, true, false>(a, qkv, o, d_o, stats, dqkv, rows, pairs, splits, st);
-  return a.dr.q ? bwd_launch<T, DH, false, true>(a, qkv, o, d_o, stats, dqkv, rows, pairs, splits, st)
-                : bwd_launch<T, DH, false, false>(a, qkv, o, d_o, stats, dqkv, rows, pairs, splits, st);
+    return a.dr.q ? bwd_launch<T, DH, true, true>(a, qkv, o, d_o, stats, dqkv, rows, pairs, units, st)
+                  : bwd_launch<T, DH, true, false>(a, qkv, o, d_o, stats, dqkv, rows, pairs, units, st);
+  return a.dr.q ? bwd_launch<T, DH, false, true>(a, qkv, o, d_o, stats, dqkv, rows, pairs, units, st)
+                : bwd_launch<T, DH, false, false>(a, qkv, o, d_o, stats, dqkv, rows, pairs, units, st);
 }
 }  // namespace
 
@@ -669,11 +681,11 @@ template <typename T> int rel_mfma_fwd(const RelArgs& a, const T* qkv, T* o, flo
   }
 }
 template <typename T>
-int rel_mfma_bwd(const RelArgs& a, const T* qkv, const T* o, const T* d_o, const float* stats, T* dqkv, float* rows, float* pairs, int splits, hipStream_t st) {
+int rel_mfma_bwd(const RelArgs& a, const T* qkv, const T* o, const T* d_o, const float* stats, T* dqkv, float* rows, float* pairs, int units, hipStream_t st) {
   switch (a.dh) {
-    case 16: return bwd_of<T, 16>(a, qkv, o, d_o, stats, dqkv, rows, pairs, splits, st);
-    case 32: return bwd_of<T, 32>(a, qkv, o, d_o, stats, dqkv, rows, pairs, splits, st);
-    case 64: return bwd_of<T, 64>(a, qkv, o, d_o, stats, dqkv, rows, pairs, splits, st);
-    default: return bwd_of<T, 128>(a, qkv, o, d_o, stats, dqkv, rows, pairs, splits, st);
+    case 16: return bwd_of<T, 16>(a, qkv, o, d_o, stats, dqkv, rows, pairs, units, st);
+    case 32: return bwd_of<T, 32>(a, qkv, o, d_o, stats, dqkv, rows, pairs, units, st);
+    case 64: return bwd_of<T, 64>(a, qkv, o, d_o, stats, dqkv, rows, pairs, units, st);
+    default: return bwd_of<T, 128>(a, qkv, o, d_o, stats, dqkv, rows, pairs, units, st);
   }
 }

@@ -97,10 +97,15 @@ __global__ void __launch_bounds__(256) plan_parts_kernel(int buckets, int* __res
   const int k = blockIdx.x * 256 + threadIdx.x;
   if (k >= buckets) return;
   int sum = 0;
-  for (int p = 0; p < kParts; ++p) {
-    const int c = count[(size_t)p * buckets + k];
-    count[(size_t)p * buckets + k] = sum;
-    sum += c;
+  for (int p0 = 0; p0 < kParts; p0 += 32) {
+    int c[32];
+#pragma unroll
+    for (int p = 0; p < 32; ++p) c[p] = count[(size_t)(p0 + p) * buckets + k];
+#pragma unroll
+    for (int p = 0; p < 32; ++p) {
+      count[(size_t)(p0 + p) * buckets + k] = sum;
+      sum += c[p];
+    }
   }
   start[k] = sum;
 }
