@@ -6,16 +6,20 @@
 // ---- generator -----------------------------------------------------------------------------------------------
 // Philox4x32 with seven rounds (J. Salmon, M. Moraes, R. Dror, D. Shaw, SC 2011), the fewest with which its authors found no
 // failing test.  A round is two 32 x 32 -> 64-bit products (v_mad_u64_u32).
-__device__ __forceinline__ unsigned xor3(unsigned a, unsigned b, unsigned c) { return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96); }
+// UNIFORM: of values that all lanes share, on the scalar unit
+template <bool UNIFORM> __device__ __forceinline__ unsigned xor3(unsigned a, unsigned b, unsigned c) {
+  return UNIFORM ? a ^ b ^ c : __builtin_amdgcn_bitop3_b32(a, b, c, 0x96);
+}
 struct RelWords { unsigned w[4]; };
 struct RelKey { unsigned k0, k1; };
+template <bool UNIFORM = false>
 __device__ __forceinline__ RelWords rel_words(unsigned c0, unsigned c1, unsigned c2, unsigned c3, RelKey k) {
 #pragma unroll
   for (int i = 0; i < 7; ++i) {
     const unsigned long long a = (unsigned long long)c0 * 0xD2511F53u, b = (unsigned long long)c2 * 0xCD9E8D57u;
-    c0 = xor3((unsigned)(b >> 32), c1, k.k0);
+    c0 = xor3<UNIFORM>((unsigned)(b >> 32), c1, k.k0);
     c1 = (unsigned)b;
-    c2 = xor3((unsigned)(a >> 32), c3, k.k1);
+    c2 = xor3<UNIFORM>((unsigned)(a >> 32), c3, k.k1);
     c3 = (unsigned)a;
     k.k0 += 0x9E3779B9u;
     k.k1 += 0xBB67AE85u;
@@ -25,7 +29,7 @@ __device__ __forceinline__ RelWords rel_words(unsigned c0, unsigned c1, unsigned
 // the key of a call site in this step
 __device__ __forceinline__ RelKey rel_key(const unsigned long long* rng, unsigned site) {
   const unsigned long long seed = rng[0], step = rng[1];
-  const RelWords r = rel_words((unsigned)step, (unsigned)(step >> 32), site, 0u, RelKey{(unsigned)seed, (unsigned)(seed >> 32)});
+  const RelWords r = rel_words<true>((unsigned)step, (unsigned)(step >> 32), site, 0u, RelKey{(unsigned)seed, (unsigned)(seed >> 32)});
   return RelKey{r.w[0], r.w[1]};
 }
 constexpr unsigned kDrawElements = 0, kDrawGroups = 1, kDrawPairs = 2;      // last word of the counter

@@ -216,45 +216,55 @@ __device__ __forceinline__ f32x16_t score_tile(const unsigned char* m, const typ
 template <int CTRL> __device__ __forceinline__ unsigned quad(unsigned v) {
   return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
 }
-constexpr int kSwap1 = 0xb1, kSwap2 = 0x4e;      // the neighbour of two, the other two of four
-// word j of this lane <-> word (lane % 4) of lane j of the four
-__device__ __forceinline__ void transpose4(unsigned (&w)[4], int lane) {
-  const bool odd = lane & 1, high = lane & 2;
-#pragma unroll
-  for (int j = 0; j < 4; j += 2) {
-    const unsigned a = quad<kSwap1>(w[j + 1]), b = quad<kSwap1>(w[j]);
-    w[j] = odd ? a : w[j];
-    w[j + 1] = odd ? w[j + 1] : b;
-  }
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const unsigned a = quad<kSwap2>(w[j + 2]), b = quad<kSwap2>(w[j]);
-    w[j] = high ? a : w[j];
-    w[j + 2] = high ? w[j + 2] : b;
-  }
+constexpr int kSwap1 = 0xb1;      // the neighbour of two
+// word j of this lane <-> word (lane % 4) of lane j of the four, with selects that read the other lane themselves (v_cndmask_b32_dpp; a move and a select
+// each otherwise).  A value that a lane crossing reads is two instructions old.
+__device__ __forceinline__ void transpose4(unsigned (&w)[4]) {
+  const unsigned long long even = 0x5555555555555555ull, low = 0x3333333333333333ull;
+  unsigned a0, a1, a2, a3, b0, b1, b2, b3;
+  asm("s_mov_b64 vcc, %12\n\t"
+      "s_nop 1\n\t"
+      "v_cndmask_b32_dpp %0, %9, %8, vcc quad_perm:[1,0,3,2] row_mask:0xf bank_mask:0xf\n\t"
+      "v_cndmask_b32_dpp %2, %11, %10, vcc quad_perm:[1,0,3,2] row_mask:0xf bank_mask:0xf\n\t"
+      "s_not_b64 vcc, vcc\n\t"
+      "v_cndmask_b32_dpp %1, %8, %9, vcc quad_perm:[1,0,3,2] row_mask:0xf bank_mask:0xf\n\t"
+      "v_cndmask_b32_dpp %3, %10, %11, vcc quad_perm:[1,0,3,2] row_mask:0xf bank_mask:0xf\n\t"
+      "s_mov_b64 vcc, %13\n\t"
+      "v_cndmask_b32_dpp %4, %2, %0, vcc quad_perm:[2,3,0,1] row_mask:0xf bank_mask:0xf\n\t"
+      "v_cndmask_b32_dpp %5, %3, %1, vcc quad_perm:[2,3,0,1] row_mask:0xf bank_mask:0xf\n\t"
+      "s_not_b64 vcc, vcc\n\t"
+      "v_cndmask_b32_dpp %6, %0, %2, vcc quad_perm:[2,3,0,1] row_mask:0xf bank_mask:0xf\n\t"
+      "v_cndmask_b32_dpp %7, %1, %3, vcc quad_perm:[2,3,0,1] row_mask:0xf bank_mask:0xf"
+      : "=&v"(a0), "=&v"(a1), "=&v"(a2), "=&v"(a3), "=&v"(b0), "=&v"(b1), "=&v"(b2), "=&v"(b3)
+      : "v"(w[0]), "v"(w[1]), "v"(w[2]), "v"(w[3]), "s"(even), "s"(low)
+      : "vcc", "scc");
+  w[0] = b0, w[1] = b1, w[2] = b2, w[3] = b3;
 }
-// Draws of a tile whose lanes are queries: word[g * 2 + jp] has those of registers g * 4 + jp * 2 (low half) and the next one.
-// t4: the lane's query / 4.
+// Draws of a tile, two to a word: register i's in half i % 2 of word i / 2.
+__device__ __forceinline__ unsigned draw_of(const unsigned (&word)[8], int i) { return i & 1 ? word[i >> 1] >> 16 : word[i >> 1] & 0xffffu; }
+// Lanes are queries: a word belongs to four queries, of which each lane has made a quarter of the calls.  t4: the lane's query / 4.
 __device__ __forceinline__ void draws_by_query(unsigned (&word)[8], int key0, unsigned t4, unsigned bh, RelKey key, int lane) {
 #pragma unroll
   for (int jp = 0; jp < 2; ++jp) {
     RelWords r = rel_words((unsigned)(key0 >> 1) + (lane & 3) * 4 + (lane >> 5) * 2 + jp, t4, bh, kDrawPairs, key);
-    transpose4(r.w, lane);
+    transpose4(r.w);
 #pragma unroll
     for (int g = 0; g < 4; ++g) word[g * 2 + jp] = r.w[g];
   }
 }
-// Draws of a tile whose lanes are keys: word[i] has that of register i in its high half.
-__device__ __forceinline__ void draws_by_key(unsigned (&word)[16], int query0, unsigned u2, unsigned bh, RelKey key, int lane) {
+// Lanes are keys: two neighbours have the halves of the same words, and each has made half of the calls.  u2: the lane's key / 2.
+__device__ __forceinline__ void draws_by_key(unsigned (&word)[8], int query0, unsigned u2, unsigned bh, RelKey key, int lane) {
   const bool odd = lane & 1;
+  const unsigned own = odd ? 0x07060302u : 0x05040100u, others = odd ? 0x05040100u : 0x07060302u;      // that half of both words
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const RelWords r = rel_words(u2, (unsigned)(query0 >> 2) + (odd ? 4 : 0) + k * 2 + (lane >> 5), bh, kDrawPairs, key);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const unsigned other = quad<kSwap1>(r.w[j]), mine = r.w[j];
-      word[k * 4 + j] = (odd ? other : mine) << (odd ? 0 : 16);
-      word[8 + k * 4 + j] = (odd ? mine : other) << (odd ? 0 : 16);
+    for (int j = 0; j < 2; ++j) {
+      const unsigned mine = __builtin_amdgcn_perm(r.w[2 * j + 1], r.w[2 * j], own);
+      const unsigned got = quad<kSwap1>(__builtin_amdgcn_perm(r.w[2 * j + 1], r.w[2 * j], others));
+      word[k * 2 + j] = odd ? got : mine;
+      word[4 + k * 2 + j] = odd ? mine : got;
     }
   }
 }
@@ -352,12 +362,8 @@ __global__ void __launch_bounds__(512, sizeof(T) == 2 && DH <= 64 ? 4 : 2) rel_m
       if (DROP) {
         unsigned word[8];
         draws_by_query(word, t * 32, (unsigned)q >> 2, (unsigned)bh, key, lane);
-        const unsigned q16 = a.dr.q << 16;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          x[2 * j] = word[j] << 16 < q16 ? 0.f : x[2 * j];
-          x[2 * j + 1] = word[j] < q16 ? 0.f : x[2 * j + 1];
-        }
+        for (int i = 0; i < 16; ++i) x[i] = draw_of(word, i) < a.dr.q ? 0.f : x[i];
       }
       D::template tn<false>(Vs, x, x, oacc, oacc, lane);
     }
@@ -446,12 +452,11 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
       f32x16_t dx = D::nt(Vs, bg, zero16(), lane);
       unsigned word[8];
       if (DROP) draws_by_query(word, t * 32, (unsigned)q >> 2, (unsigned)bh, key, lane);
-      const unsigned q16 = a.dr.q << 16;
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         p[i] = __builtin_amdgcn_exp2f(fmaf(p[i] - m, kLog2e, -L2));
         float w = 1.f;
-        if (DROP) w = (i & 1 ? word[i >> 1] : word[i >> 1] << 16) < q16 ? 0.f : a.dr.scale;
+        if (DROP) w = draw_of(word, i) < a.dr.q ? 0.f : a.dr.scale;
         dx[i] = p[i] * (DROP ? fmaf(dx[i], w, -delta) : dx[i] - delta);
       }
       if (t * 32 + 32 > n) {       // keys past the image's tokens: rows of zeros, whose probabilities may be infinite
@@ -570,10 +575,9 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
         const float* R = reinterpret_cast<const float*>(S + D::STAGE) + t % TS * 32;
         f32x16_t p = score_tile<T, DH, BIAS>(Qs, bk, table, mr, a.scale, lane);
         f32x16_t dx = D::nt(Gs, bv, zero16(), lane);
-        unsigned word[16];
+        unsigned word[8];
         if (DROP) draws_by_key(word, t * 32, (unsigned)u >> 1, (unsigned)bh, key, lane);
-        const unsigned q16 = a.dr.q << 16;
-#pragma unroll
+  #pragma unroll
         for (int i4 = 0; i4 < 4; ++i4) {
           const float* r = R + i4 * 8 + h * 4;
           const float4 m4 = *reinterpret_cast<const float4*>(r), l4 = *reinterpret_cast<const float4*>(r + D::KB), d4 = *reinterpret_cast<const float4*>(r + 2 * D::KB);
@@ -583,7 +587,7 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
             const int i = i4 * 4 + k;
             const float pp = __builtin_amdgcn_exp2f(fmaf(p[i] - mm[k], kLog2e, -ll[k]));
             if (DROP) {
-              const bool gone = word[i] < q16;
+              const bool gone = draw_of(word, i) < a.dr.q;
               p[i] = gone ? 0.f : pp;
               dx[i] = pp * fmaf(dx[i], gone ? 0.f : a.dr.scale, -dd[k]);
             } else {
