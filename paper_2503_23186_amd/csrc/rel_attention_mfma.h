@@ -12,9 +12,9 @@
 // meet in a multiply-add.  The reference is subtracted from the sum, so that tables with the lowest finite value keep their meaning; the
 // exponential's base rides in the multiply-add behind it.
 //
-// dx = P (dP - delta) with delta = sum P dP.  do . o is delta up to what rounding took off o and off the probabilities in front of it, 2^-7 of its
-// terms, which would show in the table's gradient (an fp32 sum).  The walk for dq therefore takes it as an estimate: dx' = P (dP - estimate) sums to what the
-// estimate lacks, c, so that delta = estimate + c to fp32 and dq = dx' k - c P k, for one more product of a tile; the kernels behind it get delta.
+// dx = P (dP - delta) with delta = sum P dP.  do . o is delta up to what rounding took off o and off the probabilities in front of it (2^-7 of its terms),
+// which is as exact as dq's own operands are but would show in the table's gradient, an fp32 sum.  The walk for dq takes it as an estimate; its
+// dx' = P (dP - estimate) sum to what the estimate lacks, so that the walk behind it has delta to fp32.
 //
 // Dropout: a call of the generator gives eight draws, of four queries and two keys (include/cnnk_rel.h).  With a query a lane, four neighbouring
 // lanes need the four words of the same calls: each makes a quarter of the calls and they transpose words among
@@ -70,17 +70,13 @@ template <int DH> struct Dim<bf16_t, DH> {
     for (int k = 0; k < NK; ++k) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_read(m, PLANE, lane & 31, k * 16 + (lane >> 5) * 8), o.f[k], acc, 0, 0, 0);
     return acc;
   }
-  // acc += M^T x, and acc2 += M^T y: features by own rows
-  template <bool TWO> static __device__ __forceinline__ void tn(const unsigned char* m, const f32x16_t& x, const f32x16_t& y, f32x16_t* acc, f32x16_t* acc2, int lane) {
+  // acc += M^T x: features by own rows
+  static __device__ __forceinline__ void tn(const unsigned char* m, const f32x16_t& x, f32x16_t* acc, int lane) {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const bf16x8_t xb = pack_frag(x, j), yb = TWO ? pack_frag(y, j) : xb;
+      const bf16x8_t xb = pack_frag(x, j);
 #pragma unroll
-      for (int mt = 0; mt < NM; ++mt) {
-        const bf16x8_t v = frag_read_tr(m, PLANE, mt, 16 * j, lane);
-        acc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, xb, acc[mt], 0, 0, 0);
-        if (TWO) acc2[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, yb, acc2[mt], 0, 0, 0);
-      }
+      for (int mt = 0; mt < NM; ++mt) acc[mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_read_tr(m, PLANE, mt, 16 * j, lane), xb, acc[mt], 0, 0, 0);
     }
   }
   static __device__ __forceinline__ void store(bf16_t* row, const f32x16_t* acc, int h, bool inside) { store_cols<DH>(row, acc, h, inside); }
@@ -126,7 +122,7 @@ template <int DH> struct Dim<float, DH> {
     return acc;
   }
   // A step reduces over the two rows that register i of the halves stands for, and needs no conversion.
-  template <bool TWO> static __device__ __forceinline__ void tn(const unsigned char* m, const f32x16_t& x, const f32x16_t& y, f32x16_t* acc, f32x16_t* acc2, int lane) {
+  static __device__ __forceinline__ void tn(const unsigned char* m, const f32x16_t& x, f32x16_t* acc, int lane) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int row = (i >> 2) * 8 + (lane >> 5) * 4 + (i & 3);
@@ -134,7 +130,6 @@ template <int DH> struct Dim<float, DH> {
       for (int mt = 0; mt < NM; ++mt) {
         const float v = *reinterpret_cast<const float*>(m + mt * PLANE + at(row, (lane & 31) >> 2) + (lane & 3) * 4);
         acc[mt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, x[i], acc[mt], 0, 0, 0);
-        if (TWO) acc2[mt] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, y[i], acc2[mt], 0, 0, 0);
       }
     }
   }
@@ -365,7 +360,7 @@ __global__ void __launch_bounds__(512, sizeof(T) == 2 && DH <= 64 ? 4 : 2) rel_m
 #pragma unroll
         for (int i = 0; i < 16; ++i) x[i] = draw_of(word, i) < a.dr.q ? 0.f : x[i];
       }
-      D::template tn<false>(Vs, x, x, oacc, oacc, lane);
+      D::tn(Vs, x, oacc, lane);
     }
   }
   if (q0 >= a.T) return;
@@ -385,7 +380,7 @@ __global__ void __launch_bounds__(512, sizeof(T) == 2 && DH <= 64 ? 4 : 2) rel_m
 // rows [B * heads][3][Tp], Tp = T rounded up to 64: reference, log2 of the sum relative to it (+infinity for rows without a part: their probabilities
 // come out as 0), delta.
 template <typename T, int DH, bool BIAS, bool DROP>
-__global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mfma_dq_kernel(RelArgs a, const T* __restrict__ qkv, const T* __restrict__ o,
+__global__ void __launch_bounds__(DH <= 64 ? 512 : 256, sizeof(T) == 2 && DH <= 64 ? 3 : DH <= 64 ? 2 : 1) rel_mfma_dq_kernel(RelArgs a, const T* __restrict__ qkv, const T* __restrict__ o,
                                                                             const T* __restrict__ d_o, const float* __restrict__ stats,
                                                                             T* __restrict__ dqkv, float* __restrict__ rows, int parts) {
   using D = Dim<T, DH>;
@@ -400,9 +395,9 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
   const T* base = qkv + (size_t)b * a.T * ld + head * DH;
   const size_t head0 = (size_t)b * a.T * d + head * DH;
   constexpr bool FIX = sizeof(T) == 2;      // fp32: do . o is delta
-  f32x16_t dq[D::NM], pk[D::NM];            // dx' k, P k
+  f32x16_t dq[D::NM];
 #pragma unroll
-  for (int mt = 0; mt < D::NM; ++mt) dq[mt] = pk[mt] = zero16();
+  for (int mt = 0; mt < D::NM; ++mt) dq[mt] = zero16();
   float m = 0.f, L2 = INFINITY, delta = 0.f, lack = 0.f;
   if (first < n) {
     float* table = reinterpret_cast<float*>(smem + 2 * D::STAGE);
@@ -463,7 +458,7 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
         only_here();
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (t * 32 + key_of(i, h) >= n) p[i] = dx[i] = 0.f;
+          if (t * 32 + key_of(i, h) >= n) dx[i] = 0.f;
       }
       if (FIX) {
         float add[2] = {0.f, 0.f};
@@ -471,7 +466,7 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
         for (int i = 0; i < 16; ++i) add[i & 1] += dx[i];
         lack += add[0] + add[1];
       }
-      D::template tn<FIX>(Ks, dx, p, dq, pk, lane);
+      D::tn(Ks, dx, dq, lane);
     }
   }
   if (q0 >= a.T) return;
@@ -479,7 +474,7 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
 #pragma unroll
   for (int mt = 0; mt < D::NM; ++mt)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) dq[mt][i] = q < n ? (FIX ? fmaf(-lack, pk[mt][i], dq[mt][i]) : dq[mt][i]) * a.scale : 0.f;
+    for (int i = 0; i < 16; ++i) dq[mt][i] = q < n ? dq[mt][i] * a.scale : 0.f;
   D::store(dqkv + (size_t)b * a.T * ld + head * DH + (size_t)q * ld, dq, h, q < a.T);
   if (h == 0) {
     float* r = rows + (size_t)bh * 3 * a.Tp + q;
@@ -607,8 +602,8 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
             *reinterpret_cast<float4*>(sums + (size_t)t * 1024 + k * 256) =
                 float4{was[k].x + dx[4 * k], was[k].y + dx[4 * k + 1], was[k].z + dx[4 * k + 2], was[k].w + dx[4 * k + 3]};
         }
-        D::template tn<false>(Gs, p, p, dv, dv, lane);
-        D::template tn<false>(Qs, dx, dx, dk, dk, lane);
+        D::tn(Gs, p, dv, lane);
+        D::tn(Qs, dx, dk, lane);
       }
     }
     if (u0 >= a.T) continue;

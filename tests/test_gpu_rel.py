@@ -239,9 +239,11 @@ class Case:
         want = np.where(none, 0.0, np.where(none, 0.0, ref["top"]) + ref["log"])
         close(both, want, e * (1 + np.abs(want)) + 2.0 ** -23 * np.abs(np.where(none, 0.0, ref["top"])), "statistics")
         dq, dt = self.bwd(o, m)
-        # The estimate of delta, do . o, is 2^-7 of delta's terms off (probabilities as operands 2^-8, o as stored 2^-8).  What it lacks is formed in fp32, so that the
-        # rounding of dx' = dx + P c, |c| <= 2^-7 of the terms, adds 2^-8 * 2^-7, and so does that of P in c P k.
-        d = 0.0 if self.dtype == "f32" else 2.0 ** -14
+        # dq is formed with do . o for delta, which is 2^-7 of delta's terms off in bf16 (probabilities as operands of the forward product 2^-8, o as stored 2^-8,
+        # |o| <= sum D |v|), together with the rounding of dx that has that error in it: 2^-7 (1 + 2^-8).  dk, dv and the table get delta in fp32.
+        d = np.zeros((1, 1, 3, 1))
+        d[0, 0, 0] = 0.0 if self.dtype == "f32" else 2.0 ** -7 * 1.01
+        d = np.broadcast_to(d, (self.B, self.T, 3, self.heads * self.dh)).reshape(self.B, self.T, -1)
         close(dq, ref["dqkv"], h * np.abs(ref["dqkv"]) + a * 1.01 * ref["bound_dqkv"] + (e + d) * ref["size_dqkv"] * 1.01 + 1e-30, "dqkv")
         if self.n:
             close(dt, ref["dtable"], e * ref["size_dtable"] * 1.01 + 2.0 ** -23 * np.abs(ref["dtable"]) + 1e-30, "dtable")
