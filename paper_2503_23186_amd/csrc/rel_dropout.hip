@@ -9,17 +9,18 @@ constexpr int kT = 256;
 
 __global__ void rng_advance_kernel(unsigned long long* rng, unsigned long long by) { rng[1] += by; }
 
-// eight neighbours of row `row`, times keep / (1 - p)
-__device__ __forceinline__ void drop8(float* v, size_t octet, long long row, int span, RelKey key, RelDrop dr) {
-  if (span > 0) {
-    const unsigned long long i = (unsigned long long)row / (unsigned)span;
-    const RelWords r = rel_words((unsigned)(i >> 3), (unsigned)(i >> 35), 0u, kDrawGroups, key);
+// Eight neighbours of row `row`, times keep / (1 - p).  There are fewer than 2^31 octets and rows, so that the counter's second word is 0 and
+// divisions are multiplications (12608 x 768 bf16 with a residual sum 14.9 -> 14.5 us, the gradient with its sums 12.4 -> 11.3).
+__device__ __forceinline__ void drop8(float* v, int octet, int row, FastDiv span, RelKey key, RelDrop dr) {
+  if (span.d > 0) {
+    const int i = span.div(row);
+    const RelWords r = rel_words((unsigned)i >> 3, 0u, 0u, kDrawGroups, key);
     const unsigned k = (unsigned)i & 7u, w = k < 4 ? (k < 2 ? r.w[0] : r.w[1]) : (k < 6 ? r.w[2] : r.w[3]);
     const bool dropped = ((k & 1u ? w >> 16 : w & 0xffffu)) < dr.q;
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = dropped ? 0.f : v[e] * dr.scale;
   } else {
-    const RelWords r = rel_words((unsigned)octet, (unsigned)(octet >> 32), 0u, kDrawElements, key);
+    const RelWords r = rel_words((unsigned)octet, 0u, 0u, kDrawElements, key);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const unsigned draw = e & 1 ? r.w[e >> 1] >> 16 : r.w[e >> 1] & 0xffffu;
@@ -30,35 +31,36 @@ __device__ __forceinline__ void drop8(float* v, size_t octet, long long row, int
 
 template <typename T>
 __global__ void __launch_bounds__(kT) dropout_kernel(const T* z, const float* __restrict__ bias, const T* res, const unsigned long long* __restrict__ rng,
-                                                     T* y, size_t octets, int C8, int span, unsigned site, RelDrop dr) {
+                                                     T* y, int octets, FastDiv C8, FastDiv span, unsigned site, RelDrop dr) {
   RelKey key{0u, 0u};
   if (dr.q) key = rel_key(rng, site);
-  for (size_t o = (size_t)blockIdx.x * kT + threadIdx.x; o < octets; o += (size_t)gridDim.x * kT) {
-    const long long row = (long long)(o / (unsigned)C8);
-    const int c = (int)(o - (size_t)row * C8) * 8;
+  for (long long at = (long long)blockIdx.x * kT + threadIdx.x; at < octets; at += (long long)gridDim.x * kT) {
+    const int o = (int)at;
+    int row, c;
+    C8.divmod(o, &row, &c);
     float v[8];
-    load8(z + o * 8, v);
+    load8(z + at * 8, v);
     if (bias) {
       float b[8];
-      load8(bias + c, b);
+      load8(bias + c * 8, b);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] += b[e];
     }
     if (dr.q) drop8(v, o, row, span, key, dr);
     if (res) {
       float r[8];
-      load8(res + o * 8, r);
+      load8(res + at * 8, r);
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] += r[e];
     }
-    store8(y + o * 8, v);
+    store8(y + at * 8, v);
   }
 }
 
 // The backward pass with the sums over rows: 32 column octets x 8 row lanes per workgroup, blockIdx.x = slab of 256 columns, blockIdx.y = rows.
 template <typename T>
 __global__ void __launch_bounds__(kT) dropout_sum_kernel(const T* dy, const unsigned long long* __restrict__ rng, T* dz, float* __restrict__ part,
-                                                         long long rows, int C, long long rows_per_chunk, int span, unsigned site, RelDrop dr) {
+                                                         int rows, int C, int rows_per_chunk, FastDiv span, unsigned site, RelDrop dr) {
   __shared__ float sm[8][257];
   const int oc = threadIdx.x & 31, rl = threadIdx.x >> 5, c = blockIdx.x * 256 + oc * 8;
   const long long r0 = (long long)blockIdx.y * rows_per_chunk;
@@ -67,11 +69,28 @@ __global__ void __launch_bounds__(kT) dropout_sum_kernel(const T* dy, const unsi
   if (dr.q) key = rel_key(rng, site);
   float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   if (c < C) {
-    for (long long r = r0 + rl; r < r1; r += 8) {
+    long long r = r0 + rl;
+    for (; r + 8 < r1; r += 16) {          // two rows in flight
+      float v[8], w[8];
+      const size_t at = (size_t)r * C + c, bt = at + (size_t)8 * C;
+      load8(dy + at, v);
+      load8(dy + bt, w);
+      if (dr.q) {
+        drop8(v, (int)(at >> 3), (int)r, span, key, dr);
+        drop8(w, (int)(bt >> 3), (int)r + 8, span, key, dr);
+      }
+      store8(dz + at, v);
+      store8(dz + bt, w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += v[e];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += w[e];
+    }
+    for (; r < r1; r += 8) {
       float v[8];
       const size_t at = (size_t)r * C + c;
       load8(dy + at, v);
-      if (dr.q) drop8(v, at >> 3, r, span, key, dr);
+      if (dr.q) drop8(v, (int)(at >> 3), (int)r, span, key, dr);
       store8(dz + at, v);
 #pragma unroll
       for (int e = 0; e < 8; ++e) acc[e] += v[e];
@@ -104,13 +123,21 @@ int chunks_of(long long rows, int C) {
   if (want < 1) want = 1;
   return (int)(want < by_rows ? want : by_rows);
 }
+FastDiv span_of(const cnnk_dropout_desc* d) {
+  FastDiv f;
+  f.init(d->span);
+  f.d = d->span;
+  return f;
+}
 void pass(const cnnk_dropout_desc* d, const void* z, const float* bias, const void* res, const unsigned long long* rng, void* y, RelDrop dr, hipStream_t st) {
-  const size_t octets = (size_t)d->rows * d->C / 8, blocks = (octets + kT - 1) / kT;
+  const long long octets = d->rows * d->C / 8, blocks = (octets + kT - 1) / kT;
+  FastDiv C8;
+  C8.init(d->C / 8);
   const unsigned grid = (unsigned)(blocks < 16384 ? blocks : 16384);
   if (d->dtype == CNNK_BF16)
-    dropout_kernel<bf16_t><<<grid, kT, 0, st>>>((const bf16_t*)z, bias, (const bf16_t*)res, rng, (bf16_t*)y, octets, d->C / 8, d->span, d->site, dr);
+    dropout_kernel<bf16_t><<<grid, kT, 0, st>>>((const bf16_t*)z, bias, (const bf16_t*)res, rng, (bf16_t*)y, (int)octets, C8, span_of(d), d->site, dr);
   else
-    dropout_kernel<float><<<grid, kT, 0, st>>>((const float*)z, bias, (const float*)res, rng, (float*)y, octets, d->C / 8, d->span, d->site, dr);
+    dropout_kernel<float><<<grid, kT, 0, st>>>((const float*)z, bias, (const float*)res, rng, (float*)y, (int)octets, C8, span_of(d), d->site, dr);
 }
 }  // namespace
 
@@ -152,13 +179,13 @@ extern "C" int cnnk_dropout_bwd(const cnnk_dropout_desc* d, const void* dy, cons
     return launch_status();
   }
   const int chunks = chunks_of(d->rows, d->C);
-  const long long rpc = (d->rows + chunks - 1) / chunks;
+  const int rpc = (int)((d->rows + chunks - 1) / chunks);
   const dim3 grid((d->C + 255) / 256, chunks);
   float* part = (float*)ws;
   if (d->dtype == CNNK_BF16)
-    dropout_sum_kernel<bf16_t><<<grid, kT, 0, st>>>((const bf16_t*)dy, rng, (bf16_t*)dz, part, d->rows, d->C, rpc, d->span, d->site, dr);
+    dropout_sum_kernel<bf16_t><<<grid, kT, 0, st>>>((const bf16_t*)dy, rng, (bf16_t*)dz, part, (int)d->rows, d->C, rpc, span_of(d), d->site, dr);
   else
-    dropout_sum_kernel<float><<<grid, kT, 0, st>>>((const float*)dy, rng, (float*)dz, part, d->rows, d->C, rpc, d->span, d->site, dr);
+    dropout_sum_kernel<float><<<grid, kT, 0, st>>>((const float*)dy, rng, (float*)dz, part, (int)d->rows, d->C, rpc, span_of(d), d->site, dr);
   if (launch_status() != CNNK_OK) return CNNK_ERR_HIP;
   ColumnSums sums;
   sums.count = 1;

@@ -1,0 +1,218 @@
+"""The operators of include/cnnk_rel.h together with those of cnnk_vit.h, as a training step of a transformer block uses them: against autograd in float64,
+captured into a graph, on two streams at once; and sizes that need a reference on the GPU."""
+import numpy as np
+import pytest
+import torch
+import torch.nn.functional as F
+
+from oracle import rel as R
+from util import TOL
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+SEED = 0x0123456789ABCDEF
+
+
+@pytest.fixture(scope="module")
+def K():
+    assert torch.cuda.is_available(), "the GPU tests need a GPU"
+    from paper_2503_23186_amd import rel
+    return rel
+
+
+class Block:
+    """x + drop(attention(LN(x)) Wo^T + bo), then + path(LN(.) W1^T + c1): the library's calls, forward and backward, on buffers made once."""
+
+    def __init__(self, K, dtype, B, gh, gw, heads, dh, p, lens=None, seed=0):
+        from paper_2503_23186_amd import vit
+        self.K, self.V = K, vit
+        self.B, self.T, self.heads, self.dh, self.p, self.lens = B, gh * gw + 1, heads, dh, p, lens
+        self.dim, self.rows, self.n = heads * dh, B * self.T, K.grid_buckets(gh, gw, 1)
+        self.dt, t = (K.BF16, torch.bfloat16) if dtype == "bf16" else (K.F32, torch.float32)
+        g = torch.Generator().manual_seed(seed)
+        d, rows = self.dim, self.rows
+        rand = lambda *s, k=1.0: k * torch.randn(*s, generator=g)
+        self.host = dict(x=rand(rows, d), dy=rand(rows, d), Wqkv=rand(3 * d, d, k=d ** -0.5), Wo=rand(d, d, k=d ** -0.5), W1=rand(d, d, k=d ** -0.5),
+                         g1=1 + rand(d, k=0.1), b1=rand(d, k=0.1), g2=1 + rand(d, k=0.1), b2=rand(d, k=0.1), bqkv=rand(3 * d, k=0.1), bo=rand(d, k=0.1), c1=rand(d, k=0.1),
+                         table=rand(self.n, heads, k=0.7))
+        mats = ("x", "dy", "Wqkv", "Wo", "W1")
+        self.a = {k: v.to(DEV).to(t if k in mats else torch.float32) for k, v in self.host.items()}
+        self.host = {k: v.double().cpu() for k, v in self.a.items()}
+        e = lambda *s: torch.full(s, 7.0, device=DEV, dtype=t)
+        f = lambda *s: torch.full(s, 7.0, device=DEV)
+        self.o = dict(H=e(rows, d), QKV=e(rows, 3 * d), O=e(rows, d), Z=e(rows, d), X1=e(rows, d), H2=e(rows, d), Y=e(rows, d), X2=e(rows, d), dY=e(rows, d), dH2=e(rows, d),
+                      dX1=e(rows, d), dZ=e(rows, d), dO=e(rows, d), dQKV=e(rows, 3 * d), dH=e(rows, d), dx=e(rows, d))
+        self.g = dict(dWqkv=f(3 * d, d), dWo=f(d, d), dW1=f(d, d), dg1=f(d), db1=f(d), dg2=f(d), db2=f(d), dbo=f(d), dc1=f(d), dtable=f(self.n, heads))
+        self.s1, self.s2, self.stats = f(rows, 2), f(rows, 2), f(B, heads, self.T, 2)
+        self.rng = torch.from_numpy(np.array([SEED, 40], dtype=np.uint64).view(np.int64)).to(DEV)
+        self.m = torch.empty(self.T, self.T, dtype=torch.int32, device=DEV)
+        K.cnnk_rel_buckets_grid(gh, gw, 1, self.m, torch.cuda.current_stream().cuda_stream)
+        self.plan = K.make_plan(self.m, self.n)
+        self.gl = None if lens is None else torch.tensor(lens, dtype=torch.int32, device=DEV)
+        self.ln = vit.ln_desc(rows, d, self.dt)
+        self.at = K.rel_desc(B, self.T, heads, dh, self.dt, self.n, p, 0)
+        self.d1, self.d2 = K.dropout_desc(rows, d, self.dt, p, 1), K.dropout_desc(rows, d, self.dt, 0.5, 2, self.T)
+        need = max(vit.cnnk_layernorm_workspace_bytes(self.ln), K.cnnk_rel_attention_workspace_bytes(self.at), K.cnnk_dropout_workspace_bytes(self.d1),
+                   vit.cnnk_linear_workspace_bytes(rows, d, 3 * d, self.dt), vit.cnnk_linear_workspace_bytes(rows, 3 * d, d, self.dt), 256)
+        self.ws = torch.empty(need, dtype=torch.uint8, device=DEV)
+
+    def step(self, st=None):
+        K, V, a, o, g, ws, nb = self.K, self.V, self.a, self.o, self.g, self.ws, self.ws.numel()
+        r, d, dt, st = self.rows, self.dim, self.dt, torch.cuda.current_stream().cuda_stream if st is None else st
+        V.cnnk_layernorm_fwd(self.ln, a["x"], a["g1"], a["b1"], o["H"], self.s1, st)
+        V.cnnk_linear_fwd(r, d, 3 * d, dt, o["H"], a["Wqkv"], a["bqkv"], V.ACT_NONE, None, o["QKV"], ws, nb, st)
+        K.cnnk_rel_attention_fwd(self.at, o["QKV"], a["table"], self.plan, self.gl, self.rng, o["O"], self.stats, st)
+        V.cnnk_linear_fwd(r, d, d, dt, o["O"], a["Wo"], None, V.ACT_NONE, None, o["Z"], ws, nb, st)
+        K.cnnk_dropout_fwd(self.d1, o["Z"], a["bo"], a["x"], self.rng, o["X1"], st)
+        V.cnnk_layernorm_fwd(self.ln, o["X1"], a["g2"], a["b2"], o["H2"], self.s2, st)
+        V.cnnk_linear_fwd(r, d, d, dt, o["H2"], a["W1"], None, V.ACT_NONE, None, o["Y"], ws, nb, st)
+        K.cnnk_dropout_fwd(self.d2, o["Y"], a["c1"], o["X1"], self.rng, o["X2"], st)
+        K.cnnk_dropout_bwd(self.d2, a["dy"], self.rng, o["dY"], g["dc1"], ws, nb, st)
+        V.cnnk_linear_wgrad(r, d, d, dt, o["H2"], o["dY"], g["dW1"], ws, nb, st)
+        V.cnnk_linear_dgrad(r, d, d, dt, o["dY"], a["W1"], o["dH2"], ws, nb, st)
+        V.cnnk_layernorm_bwd(self.ln, o["dH2"], o["X1"], a["g2"], self.s2, a["dy"], o["dX1"], g["dg2"], g["db2"], ws, nb, st)
+        K.cnnk_dropout_bwd(self.d1, o["dX1"], self.rng, o["dZ"], g["dbo"], ws, nb, st)
+        V.cnnk_linear_wgrad(r, d, d, dt, o["O"], o["dZ"], g["dWo"], ws, nb, st)
+        V.cnnk_linear_dgrad(r, d, d, dt, o["dZ"], a["Wo"], o["dO"], ws, nb, st)
+        K.cnnk_rel_attention_bwd(self.at, o["QKV"], o["O"], o["dO"], a["table"], self.plan, self.gl, self.rng, self.stats, o["dQKV"], g["dtable"], ws, nb, st)
+        V.cnnk_linear_wgrad(r, d, 3 * d, dt, o["H"], o["dQKV"], g["dWqkv"], ws, nb, st)
+        V.cnnk_linear_dgrad(r, d, 3 * d, dt, o["dQKV"], a["Wqkv"], o["dH"], ws, nb, st)
+        V.cnnk_layernorm_bwd(self.ln, o["dH"], a["x"], a["g1"], self.s1, o["dX1"], o["dx"], g["dg1"], g["db1"], ws, nb, st)
+        K.cnnk_rng_advance(self.rng, 1, st)
+
+    def results(self):
+        return [t.clone() for t in (self.o["X2"], self.o["dx"], *self.g.values())]
+
+    def reference(self, step):
+        h = {k: v.clone().requires_grad_(k != "dy") for k, v in self.host.items()}
+        B, T, H, dh = self.B, self.T, self.heads, self.dh
+        key = lambda site: R.site_key(SEED, step, site)
+        keep = torch.from_numpy(R.keep_pairs(B, H, T, self.p, key(0))) if self.p else 1.0
+        k1 = torch.from_numpy(R.keep_dropout(self.rows, self.dim, self.p, 0, key(1)))
+        k2 = torch.from_numpy(np.ascontiguousarray(R.keep_dropout(self.rows, self.dim, 0.5, T, key(2))))
+        q, k, v = F.linear(F.layer_norm(h["x"], (self.dim,), h["g1"], h["b1"], 1e-6), h["Wqkv"], h["bqkv"]).reshape(B, T, 3, H, dh).permute(2, 0, 3, 1, 4)
+        x = q @ k.transpose(-1, -2) / dh ** 0.5 + h["table"][self.m.cpu().long()].permute(2, 0, 1)
+        n = torch.tensor(self.lens if self.lens is not None else [T] * B)
+        inside = torch.arange(T)[None] < n[:, None]
+        A = torch.softmax(x.masked_fill(~inside[:, None, None, :], -1e300), -1) * inside[:, None, :, None]
+        O = ((A * keep) @ v).permute(0, 2, 1, 3).reshape(B * T, -1)
+        X1 = h["x"] + k1 * (F.linear(O, h["Wo"]) + h["bo"])
+        X2 = X1 + k2 * (F.linear(F.layer_norm(X1, (self.dim,), h["g2"], h["b2"], 1e-6), h["W1"]) + h["c1"])
+        X2.backward(h["dy"])
+        names = {"dWqkv": "Wqkv", "dWo": "Wo", "dW1": "W1", "dg1": "g1", "db1": "b1", "dg2": "g2", "db2": "b2", "dbo": "bo", "dc1": "c1", "dtable": "table"}
+        return [X2.detach(), h["x"].grad] + [h[names[k]].grad for k in self.g]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,gh,gw,heads,dh,p,lens", [(3, 4, 4, 2, 64, 0.1, None), (2, 9, 7, 4, 32, 0.2, None), (4, 6, 5, 2, 64, 0.1, [31, 7, 0, 20]), (2, 14, 14, 3, 64, 0.0, None)])
+def test_block_against_autograd(K, dtype, B, gh, gw, heads, dh, p, lens):
+    """The framework's bars for whole tensors: 1e-4 of the largest value in fp32, 2e-2 in bf16.  (Image 2 of the padded batch has no tokens.)"""
+    b = Block(K, dtype, B, gh, gw, heads, dh, p, lens)
+    b.step()
+    for got, want, name in zip(b.results(), b.reference(40), ["X2", "dx"] + list(b.g)):
+        got = got.double().cpu()
+        assert torch.isfinite(got).all(), name
+        err = float((got - want).abs().max() / want.abs().max())
+        assert err <= TOL[dtype], (name, err)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_block_in_a_captured_graph(K, dtype):
+    """Every replay, with eager work between, gives what the eager step of the same state gives, bit for bit."""
+    b = Block(K, dtype, 3, 9, 9, 2, 64, 0.2, [82, 50, 3])
+    start = b.rng.clone()
+    want = []
+    for _ in range(4):
+        b.step()
+        want.append(b.results())
+    b.rng.copy_(start)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        b.step()
+    for k in range(4):
+        for t in (*b.o.values(), *b.g.values(), b.stats):
+            t.fill_(3.0)
+        b.ws.fill_(255)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for x, y in zip(b.results(), want[k]):
+            assert torch.equal(x, y), k
+        (b.a["x"].float() * 2).sum().item()
+
+
+def test_two_blocks_on_two_streams(K):
+    """Calls that share a plan and nothing else, at the same time on two streams."""
+    one, two = Block(K, "bf16", 4, 14, 14, 3, 64, 0.1, seed=1), Block(K, "bf16", 4, 14, 14, 3, 64, 0.1, seed=2)
+    two.plan = one.plan
+    start = one.rng.clone()
+    one.step(), two.step()
+    want = one.results(), two.results()
+    one.rng.copy_(start), two.rng.copy_(start)
+    torch.cuda.synchronize()
+    streams = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(3):
+        for b, s in zip((one, two), streams):
+            with torch.cuda.stream(s):
+                b.rng.copy_(start)
+                b.step()
+    torch.cuda.synchronize()
+    for b, w in zip((one, two), want):
+        for x, y in zip(b.results(), w):
+            assert torch.equal(x, y)
+
+
+# ---- sizes that need a reference on the GPU ------------------------------------------------------------------------------------
+
+def reference64(qkv, heads, dh, table, bucket, g):
+    """float64 on the GPU, one image, head by head; autograd."""
+    T = qkv.shape[0]
+    x = qkv.double().reshape(T, 3, heads, dh)
+    o, d, dt = torch.zeros(T, heads, dh, dtype=torch.float64, device=DEV), torch.zeros_like(x), None if table is None else torch.zeros_like(table, dtype=torch.float64)
+    for h in range(heads):
+        q, k, v = (x[:, i, h].clone().requires_grad_() for i in range(3))
+        s = q @ k.t() / dh ** 0.5
+        leaf = [q, k, v]
+        if table is not None:
+            w = table[:, h].double().clone().requires_grad_()
+            leaf.append(w)
+            s = s + w[bucket.long().clamp(0, table.shape[0] - 1)]
+            s = s.masked_fill((bucket < 0) | (bucket >= table.shape[0]), -1e300)
+        out = torch.softmax(s, -1) @ v
+        grads = torch.autograd.grad(out, leaf, g[:, h * dh:(h + 1) * dh].double())
+        o[:, h] = out.detach()
+        for i in range(3):
+            d[:, i, h] = grads[i]
+        if table is not None:
+            dt[:, h] = grads[3]
+    return o.reshape(T, -1), d.reshape(T, -1), dt
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,heads,dh,buckets", [(300, 2, 64, 16382), (300, 1, 128, 16382), (290, 3, 16, 16000), (2049, 1, 32, 3), (4100, 1, 64, 16129), (8192, 1, 16, 40),
+                                                (16384, 1, 16, 0), (5000, 1, 128, 0)])
+def test_large_tables_and_long_sequences(K, dtype, T, heads, dh, buckets):
+    """Norm of the error over the norm of the result: in bf16 the roundings of operands and results, 2^-8 each at most and independent, in fp32 sums of T terms."""
+    gen = torch.Generator(device=DEV).manual_seed(T + dh)
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    rand = lambda *s: torch.randn(*s, generator=gen, device=DEV)
+    qkv, g = rand(T, 3 * heads * dh).to(t), rand(T, heads * dh).to(t)
+    table = plan = bucket = dt = None
+    if buckets:
+        table = rand(buckets, heads)
+        bucket = torch.randint(-1, buckets, (T, T), generator=gen, device=DEV, dtype=torch.int32)
+        plan, dt = K.make_plan(bucket, buckets), torch.full_like(table, 7.0)
+    d = K.rel_desc(1, T, heads, dh, K.BF16 if dtype == "bf16" else K.F32, buckets, 0.0, 0)
+    st = torch.cuda.current_stream().cuda_stream
+    o, stats, dq = torch.full((T, heads * dh), 7.0, device=DEV, dtype=t), torch.empty(1, heads, T, 2, device=DEV), torch.full_like(qkv, 7.0)
+    ws = torch.empty(K.cnnk_rel_attention_workspace_bytes(d), dtype=torch.uint8, device=DEV)
+    K.cnnk_rel_attention_fwd(d, qkv, table, plan, None, None, o, stats, st)
+    K.cnnk_rel_attention_bwd(d, qkv, o, g, table, plan, None, None, stats, dq, dt, ws, ws.numel(), st)
+    wo, wd, wt = reference64(qkv, heads, dh, table, bucket, g)
+    off = lambda a, b: float((a.double() - b).norm() / b.norm())
+    half = 2.0 ** -8 if dtype == "bf16" else (T + 64) * 2.0 ** -24
+    assert off(o, wo) <= half and off(dq, wd) <= 2 * half
+    if buckets:
+        assert off(dt, wt) <= (T + 64) * 2.0 ** -24 + 2.0 ** -17
