@@ -5,6 +5,7 @@
 struct RelArgs {
   int B, T, Tp, heads, dh, NT, buckets;      // Tp: T rounded up to 64, NT: blocks of 32
   float scale;                               // 1 / sqrt(dh)
+  float down, up;                            // log2 of what probabilities are divided by while they are summed, and 2^down
   unsigned site;
   RelDrop dr;
   const float* table;

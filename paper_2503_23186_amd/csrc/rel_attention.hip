@@ -99,6 +99,10 @@ RelArgs args_of(const cnnk_rel_desc* d, RelDrop dr, const float* table, const vo
   a.NT = (d->T + 31) / 32;
   a.buckets = d->buckets;
   a.scale = (float)(1.0 / sqrt((double)d->dh));
+  int down = d->dtype == CNNK_BF16 ? 8 : 0;
+  while (1 << (down - (d->dtype == CNNK_BF16 ? 8 : 0)) < d->T) ++down;
+  a.down = (float)down;
+  a.up = (float)(1 << down);
   a.site = d->site;
   a.dr = dr;
   a.table = table;

@@ -26,9 +26,10 @@
 
 namespace {
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
-// Probabilities are summed as 2^((x - m) log2 e - kDown), where m is a reference that a row's largest score so far passes by at most kSlack:
-// none is above 2^-14, so that sums over 16384 keys stay below the largest value.
-constexpr float kSlack = 5.5f, kDown = 22.f;
+// Probabilities are summed as 2^((x - m) log2 e - down), where m is a reference that a row's largest score so far passes by at most `slack`, and 2^down is T times
+// 2^(slack log2 e): sums over T keys stay below the largest value.  A reference that is raised lazily saves rescaling; fp32 storage, whose time the
+// products take, has none of it, since the bits of `down` are missing in the exponent's fraction.
+template <typename T> constexpr float kSlack = sizeof(T) == 2 ? 5.5f : 0.f;
 
 // ---- storage types -----------------------------------------------------------------------------------------------------------
 // Dim<T, DH>: the LDS layout of a stage's two matrices and the products with them.  EXACT: 1 / sqrt(DH) goes into one operand without a rounding that
@@ -336,7 +337,7 @@ __global__ void __launch_bounds__(512, sizeof(T) == 2 && DH <= 64 ? 4 : 2) rel_m
 #pragma unroll
       for (int i = 1; i < 16; ++i) tm = fmaxf(tm, x[i]);
       tm = both_halves_max(tm);
-      if (__any(tm > m + kSlack)) {
+      if (__any(tm > m + kSlack<T>)) {
         const float mn = fmaxf(m, tm);
         const float f = m == mn ? 1.f : __builtin_amdgcn_exp2f((m - mn) * kLog2e);      // also where both are -infinity
         l *= f;
@@ -350,7 +351,7 @@ __global__ void __launch_bounds__(512, sizeof(T) == 2 && DH <= 64 ? 4 : 2) rel_m
       float add[2] = {0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        x[i] = __builtin_amdgcn_exp2f(fmaf(x[i] - ref, kLog2e, -kDown));
+        x[i] = __builtin_amdgcn_exp2f(fmaf(x[i] - ref, kLog2e, -a.down));
         add[i & 1] += x[i];
       }
       l += add[0] + add[1];
@@ -373,7 +374,7 @@ __global__ void __launch_bounds__(512, sizeof(T) == 2 && DH <= 64 ? 4 : 2) rel_m
     for (int i = 0; i < 16; ++i) oacc[mt][i] = any ? oacc[mt][i] * inv : 0.f;
   D::store(o + ((size_t)b * a.T + q) * d + head * DH, oacc, h, q < a.T);
   if (stats && h == 0 && q < a.T)
-    *reinterpret_cast<float2*>(stats + ((size_t)bh * a.T + q) * 2) = any ? float2{m, kLn2 * (__builtin_amdgcn_logf(l) + kDown)} : float2{-INFINITY, 0.f};
+    *reinterpret_cast<float2*>(stats + ((size_t)bh * a.T + q) * 2) = any ? float2{m, kLn2 * __builtin_amdgcn_logf(l * a.up)} : float2{-INFINITY, 0.f};
 }
 
 // ---- backward: dq, and for the kernel behind it the rows' statistics and delta -----------------------------------------------
