@@ -52,6 +52,9 @@ static inline bool rel_aligned(const void* p, size_t a) { return ((size_t)p & (a
 //   by_query  a lane a query (column), its registers keys    u16 [NT][NT][64][16]
 //   by_key    a lane a key, its registers queries, block (u / 32, t / 32)
 // An entry is 4 x bucket, the byte offset into a head's table in LDS; 4 x buckets for masked pairs and for padding, where that table holds -infinity.
+//   live_query, live_key   u64 [NT][4]: bit k of a block of queries (keys): its pairs with block k of the others are not all masked.  The walks
+//             leave the others out.
+//   dead      int: how many blocks that are
 // What reduces dx of the pairs, summed over images, to buckets.  These sums lie in blocks as in by_key, in a block registers in fours [4][64 lanes][4].
 //   order     u16 [NT][NT][64][16]: a block's pairs sorted by bucket (masked ones last), sixteen to a lane: their bytes in the block
 //   ends      u32 [NT][NT][64]: low half: which of a lane's sixteen end a run of one bucket; high half: runs of the lanes before
@@ -59,7 +62,7 @@ static inline bool rel_aligned(const void* p, size_t a) { return ((size_t)p & (a
 //   start     int [buckets + 1]: where a bucket's runs begin in
 //   list      int [T * T at most]: places of its runs, in the order of the blocks
 constexpr int kRelMaxT = 8192, kRelMaxBuckets = 16382;
-struct RelPlan { size_t by_query, by_key, order, ends, start, list, bytes; };
+struct RelPlan { size_t by_query, by_key, order, ends, live_query, live_key, dead, start, list, bytes; };
 static inline RelPlan rel_plan_layout(int T, int buckets) {
   const size_t NT = (T + 31) / 32, map = NT * NT * 2048;
   RelPlan p;
@@ -67,7 +70,10 @@ static inline RelPlan rel_plan_layout(int T, int buckets) {
   p.by_key = map;
   p.order = 2 * map;
   p.ends = 3 * map;
-  p.start = p.ends + NT * NT * 256;
+  p.live_query = p.ends + NT * NT * 256;
+  p.live_key = p.live_query + NT * 32;
+  p.dead = p.live_query + align_up(NT * 64, 256);
+  p.start = p.dead + 256;
   p.list = p.start + align_up((size_t)(buckets + 1) * 4, 256);
   p.bytes = p.list + align_up((size_t)T * T * 4, 256);
   return p;

@@ -11,6 +11,8 @@ struct RelArgs {
   const float* table;
   const unsigned short *by_query, *by_key, *order;
   const unsigned* ends;
+  const int* dead;
+  const unsigned long long *live_query, *live_key;
   const int *start, *list, *lens;
   const unsigned long long* rng;
 };

@@ -14,6 +14,7 @@ __global__ void __launch_bounds__(256) rel_runs_kernel(RelArgs a, float* pairs, 
   const uint4* op = reinterpret_cast<const uint4*>(a.order + (size_t)block * 1024 + lane * 16);
   const uint4 o0 = op[0], o1 = op[1];
   const unsigned w[8] = {o0.x, o0.y, o0.z, o0.w, o1.x, o1.y, o1.z, o1.w}, ends = a.ends[(size_t)block * 64 + lane];
+  if (!__any(ends & 0xffffu)) return;       // masked pairs only: no walk has been there
   const int h1 = min(a.heads, ((int)blockIdx.y + 1) * heads_of);
   for (int h = blockIdx.y * heads_of; h < h1; ++h) {
     float* m = pairs + ((size_t)h * blocks + block) * 1024;
@@ -108,6 +109,8 @@ RelArgs args_of(const cnnk_rel_desc* d, RelDrop dr, const float* table, const vo
   a.table = table;
   a.by_query = a.by_key = a.order = nullptr;
   a.ends = nullptr;
+  a.live_query = a.live_key = nullptr;
+  a.dead = nullptr;
   a.start = a.list = nullptr;
   a.lens = lens;
   a.rng = rng;
@@ -117,6 +120,9 @@ RelArgs args_of(const cnnk_rel_desc* d, RelDrop dr, const float* table, const vo
     a.by_key = (const unsigned short*)((const char*)plan + at.by_key);
     a.order = (const unsigned short*)((const char*)plan + at.order);
     a.ends = (const unsigned*)((const char*)plan + at.ends);
+    a.dead = (const int*)((const char*)plan + at.dead);
+    a.live_query = (const unsigned long long*)((const char*)plan + at.live_query);
+    a.live_key = (const unsigned long long*)((const char*)plan + at.live_key);
     a.start = (const int*)((const char*)plan + at.start);
     a.list = (const int*)((const char*)plan + at.list);
   }

@@ -208,6 +208,47 @@ __device__ __forceinline__ f32x16_t score_tile(const unsigned char* m, const typ
   return x;
 }
 
+// ---- blocks that are not all masked ----------------------------------------------------------------------------------------------
+// Which blocks of the other side a wavefront's block, and any of its workgroup's, has pairs with: in LDS, since few maps leave any out.
+constexpr int kLiveBytes = 9 * 32;
+struct Live {
+  const unsigned long long* w;       // bits of the wavefront's block
+  const unsigned long long* all;     // of the workgroup's together
+  bool some;                         // blocks are left out
+};
+template <bool BIAS>
+__device__ __forceinline__ Live live_start(unsigned char* lds, const unsigned long long* p, int dead, int block0, int NT, int wave, int lane) {
+  unsigned long long* m = reinterpret_cast<unsigned long long*>(lds);
+  Live l = {m + wave * 4, m + 32, BIAS && __builtin_amdgcn_readfirstlane(dead) != 0};
+  if (l.some) {
+    if (threadIdx.x < 32) {
+      const unsigned long long v = block0 + (lane >> 2) < NT ? p[(size_t)block0 * 4 + lane] : 0;      // word lane % 4 of block lane / 4
+      m[lane] = v;
+      unsigned lo = (unsigned)v, hi = (unsigned)(v >> 32);
+#pragma unroll
+      for (int d = 4; d < 32; d *= 2) {
+        lo |= __shfl_xor(lo, d, 64);
+        hi |= __shfl_xor(hi, d, 64);
+      }
+      if (lane < 4) m[32 + lane] = (unsigned long long)hi << 32 | lo;
+    }
+    workgroup_barrier();
+  }
+  return l;
+}
+// the first of blocks from .. end - 1 that is there, end if none is
+__device__ __forceinline__ int live_next(const unsigned long long* w, bool some, int from, int end) {
+  if (!some) return min(from, end);
+  while (from < end) {
+    const unsigned long long v = w[from >> 6];
+    const unsigned long long m =
+        ((unsigned long long)(unsigned)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)v)) >> (from & 63);
+    if (m) return min(end, from + (int)__builtin_ctzll(m));
+    from = (from | 63) + 1;
+  }
+  return end;
+}
+
 // ---- dropout ---------------------------------------------------------------------------------------------------------------
 template <int CTRL> __device__ __forceinline__ unsigned quad(unsigned v) {
   return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
@@ -299,11 +340,14 @@ __global__ void __launch_bounds__(512, sizeof(T) == 2 && DH <= 64 ? 4 : 2) rel_m
     float* table = reinterpret_cast<float*>(smem + 2 * D::STAGE);
     Stager<T, DH> st;
     st.init(base + d, base + 2 * d, (unsigned)(ld * sizeof(T)), (unsigned)(ld * sizeof(T)), n, lane);
-    st.load(0, 0, wave, waves);
+    st.load(0, 0, wave, waves);      // whether it is needed or not: which stages are is on its way
     const bool mine = q0 < n;
+    const int tiles = (n + 31) >> 5, stages = (tiles + TS - 1) / TS;
     const unsigned short* map = BIAS ? a.by_query + (size_t)(q0 >> 5) * a.NT * 1024 : nullptr;
     MapRegs mr, next;
+    int dead = 0;
     if (BIAS) {
+      dead = *a.dead;
       if (mine) map_load(next, map, 0, lane);
       table_load(2 * D::STAGE, table, a, head, wave, waves, lane);
     }
@@ -312,56 +356,66 @@ __global__ void __launch_bounds__(512, sizeof(T) == 2 && DH <= 64 ? 4 : 2) rel_m
     D::scale(bq);
     RelKey key{0u, 0u};
     if (DROP) key = rel_key(a.rng, a.site);
-    const int tiles = (n + 31) >> 5;
-    for (int t = 0; t < tiles; ++t) {
-      const int stage = t / TS;
-      if (t % TS == 0) {
-        wait_vm<0>();
-        workgroup_barrier();
-        if (t + TS < tiles) st.load(t * 32 + D::KB, (stage + 1 & 1) * D::STAGE, wave, waves);
-      }
-      if (!mine) continue;
-      if (BIAS) {
-        mr = next;
-        if (t + 1 < tiles) map_load(next, map, t + 1, lane);
-      }
-      const unsigned char *Ks = smem + (stage & 1) * D::STAGE + t % TS * TILE, *Vs = Ks + D::MAT;
-      f32x16_t x = score_tile<T, DH, BIAS>(Ks, bq, table, mr, a.scale, lane);
-      if (t * 32 + 32 > n) {
-        only_here();
+    // stages that one of the workgroup's blocks needs, and of them the tiles that this wavefront's does
+    const Live live = live_start<BIAS>(reinterpret_cast<unsigned char*>(table + a.buckets + 1 + (a.buckets + 1 & 1)), a.live_query, dead, first >> 5, a.NT, wave, lane);
+    auto tile_from = [&](int t) __attribute__((always_inline)) { return live_next(live.w, live.some, t, tiles); };
+    auto stage_from = [&](int k) __attribute__((always_inline)) {
+      const int t = live_next(live.all, live.some, k * TS, tiles);
+      return t < tiles ? t / TS : stages;
+    };
+    int tn = mine ? tile_from(0) : tiles;
+    if (BIAS && tn > 0 && tn < tiles) map_load(next, map, tn, lane);
+    for (int stage = 0, buf = 0; stage < stages; buf ^= 1) {
+      wait_vm<0>();
+      workgroup_barrier();
+      const int then = stage_from(stage + 1);
+      if (then < stages) st.load(then * D::KB, (buf ^ 1) * D::STAGE, wave, waves);
+      while (tn < min(tiles, (stage + 1) * TS)) {
+        const int t = tn;
+        tn = tile_from(t + 1);
+        if (BIAS) {
+          mr = next;
+          if (tn < tiles) map_load(next, map, tn, lane);
+        }
+        const unsigned char *Ks = smem + buf * D::STAGE + (t - stage * TS) * TILE, *Vs = Ks + D::MAT;
+        f32x16_t x = score_tile<T, DH, BIAS>(Ks, bq, table, mr, a.scale, lane);
+        if (t * 32 + 32 > n) {
+          only_here();
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (t * 32 + key_of(i, h) >= n) x[i] = -INFINITY;
+          for (int i = 0; i < 16; ++i)
+            if (t * 32 + key_of(i, h) >= n) x[i] = -INFINITY;
+        }
+        float tm = x[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) tm = fmaxf(tm, x[i]);
+        tm = both_halves_max(tm);
+        if (__any(tm > m + kSlack<T>)) {
+          const float mn = fmaxf(m, tm);
+          const float f = m == mn ? 1.f : __builtin_amdgcn_exp2f((m - mn) * kLog2e);      // also where both are -infinity
+          l *= f;
+#pragma unroll
+          for (int mt = 0; mt < D::NM; ++mt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) oacc[mt][i] *= f;
+          m = mn;
+        }
+        const float ref = m > -INFINITY ? m : 0.f;
+        float add[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          x[i] = __builtin_amdgcn_exp2f(fmaf(x[i] - ref, kLog2e, -a.down));
+          add[i & 1] += x[i];
+        }
+        l += add[0] + add[1];
+        if (DROP) {
+          unsigned word[8];
+          draws_by_query(word, t * 32, (unsigned)q >> 2, (unsigned)bh, key, lane);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) x[i] = draw_of(word, i) < a.dr.q ? 0.f : x[i];
+        }
+        D::tn(Vs, x, oacc, lane);
       }
-      float tm = x[0];
-#pragma unroll
-      for (int i = 1; i < 16; ++i) tm = fmaxf(tm, x[i]);
-      tm = both_halves_max(tm);
-      if (__any(tm > m + kSlack<T>)) {
-        const float mn = fmaxf(m, tm);
-        const float f = m == mn ? 1.f : __builtin_amdgcn_exp2f((m - mn) * kLog2e);      // also where both are -infinity
-        l *= f;
-#pragma unroll
-        for (int mt = 0; mt < D::NM; ++mt)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) oacc[mt][i] *= f;
-        m = mn;
-      }
-      const float ref = m > -INFINITY ? m : 0.f;
-      float add[2] = {0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        x[i] = __builtin_amdgcn_exp2f(fmaf(x[i] - ref, kLog2e, -a.down));
-        add[i & 1] += x[i];
-      }
-      l += add[0] + add[1];
-      if (DROP) {
-        unsigned word[8];
-        draws_by_query(word, t * 32, (unsigned)q >> 2, (unsigned)bh, key, lane);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = draw_of(word, i) < a.dr.q ? 0.f : x[i];
-      }
-      D::tn(Vs, x, oacc, lane);
+      stage = then;
     }
   }
   if (q0 >= a.T) return;
@@ -404,11 +458,14 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, sizeof(T) == 2 && DH <= 
     float* table = reinterpret_cast<float*>(smem + 2 * D::STAGE);
     Stager<T, DH> st;
     st.init(base + d, base + 2 * d, (unsigned)(ld * sizeof(T)), (unsigned)(ld * sizeof(T)), n, lane);
-    st.load(0, 0, wave, waves);
+    st.load(0, 0, wave, waves);      // whether it is needed or not: which stages are is on its way
     const bool mine = q0 < n;
+    const int tiles = (n + 31) >> 5, stages = (tiles + TS - 1) / TS;
     const unsigned short* map = BIAS ? a.by_query + (size_t)(q0 >> 5) * a.NT * 1024 : nullptr;
     MapRegs mr, next;
+    int dead = 0;
     if (BIAS) {
+      dead = *a.dead;
       if (mine) map_load(next, map, 0, lane);
       table_load(2 * D::STAGE, table, a, head, wave, waves, lane);
     }
@@ -430,44 +487,54 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, sizeof(T) == 2 && DH <= 
     }
     RelKey key{0u, 0u};
     if (DROP) key = rel_key(a.rng, a.site);
-    const int tiles = (n + 31) >> 5;
-    for (int t = 0; t < tiles; ++t) {
-      const int stage = t / TS;
-      if (t % TS == 0) {
-        wait_vm<0>();
-        workgroup_barrier();
-        if (t + TS < tiles) st.load(t * 32 + D::KB, (stage + 1 & 1) * D::STAGE, wave, waves);
-      }
-      if (!mine) continue;
-      if (BIAS) {
-        mr = next;
-        if (t + 1 < tiles) map_load(next, map, t + 1, lane);
-      }
-      const unsigned char *Ks = smem + (stage & 1) * D::STAGE + t % TS * TILE, *Vs = Ks + D::MAT;
-      f32x16_t p = score_tile<T, DH, BIAS>(Ks, bq, table, mr, a.scale, lane);
-      f32x16_t dx = D::nt(Vs, bg, zero16(), lane);
-      unsigned word[8];
-      if (DROP) draws_by_query(word, t * 32, (unsigned)q >> 2, (unsigned)bh, key, lane);
+    // stages that one of the workgroup's blocks needs, and of them the tiles that this wavefront's does
+    const Live live = live_start<BIAS>(reinterpret_cast<unsigned char*>(table + a.buckets + 1 + (a.buckets + 1 & 1)), a.live_query, dead, first >> 5, a.NT, wave, lane);
+    auto tile_from = [&](int t) __attribute__((always_inline)) { return live_next(live.w, live.some, t, tiles); };
+    auto stage_from = [&](int k) __attribute__((always_inline)) {
+      const int t = live_next(live.all, live.some, k * TS, tiles);
+      return t < tiles ? t / TS : stages;
+    };
+    int tn = mine ? tile_from(0) : tiles;
+    if (BIAS && tn > 0 && tn < tiles) map_load(next, map, tn, lane);
+    for (int stage = 0, buf = 0; stage < stages; buf ^= 1) {
+      wait_vm<0>();
+      workgroup_barrier();
+      const int then = stage_from(stage + 1);
+      if (then < stages) st.load(then * D::KB, (buf ^ 1) * D::STAGE, wave, waves);
+      while (tn < min(tiles, (stage + 1) * TS)) {
+        const int t = tn;
+        tn = tile_from(t + 1);
+        if (BIAS) {
+          mr = next;
+          if (tn < tiles) map_load(next, map, tn, lane);
+        }
+        const unsigned char *Ks = smem + buf * D::STAGE + (t - stage * TS) * TILE, *Vs = Ks + D::MAT;
+        f32x16_t p = score_tile<T, DH, BIAS>(Ks, bq, table, mr, a.scale, lane);
+        f32x16_t dx = D::nt(Vs, bg, zero16(), lane);
+        unsigned word[8];
+        if (DROP) draws_by_query(word, t * 32, (unsigned)q >> 2, (unsigned)bh, key, lane);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(fmaf(p[i] - m, kLog2e, -L2));
-        float w = 1.f;
-        if (DROP) w = draw_of(word, i) < a.dr.q ? 0.f : a.dr.scale;
-        dx[i] = p[i] * (DROP ? fmaf(dx[i], w, -delta) : dx[i] - delta);
-      }
-      if (t * 32 + 32 > n) {       // keys past the image's tokens: rows of zeros, whose probabilities may be infinite
-        only_here();
+        for (int i = 0; i < 16; ++i) {
+          p[i] = __builtin_amdgcn_exp2f(fmaf(p[i] - m, kLog2e, -L2));
+          float w = 1.f;
+          if (DROP) w = draw_of(word, i) < a.dr.q ? 0.f : a.dr.scale;
+          dx[i] = p[i] * (DROP ? fmaf(dx[i], w, -delta) : dx[i] - delta);
+        }
+        if (t * 32 + 32 > n) {       // keys past the image's tokens: rows of zeros, whose probabilities may be infinite
+          only_here();
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (t * 32 + key_of(i, h) >= n) dx[i] = 0.f;
-      }
-      if (FIX) {
-        float add[2] = {0.f, 0.f};
+          for (int i = 0; i < 16; ++i)
+            if (t * 32 + key_of(i, h) >= n) dx[i] = 0.f;
+        }
+        if (FIX) {
+          float add[2] = {0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < 16; ++i) add[i & 1] += dx[i];
-        lack += add[0] + add[1];
+          for (int i = 0; i < 16; ++i) add[i & 1] += dx[i];
+          lack += add[0] + add[1];
+        }
+        D::tn(Ks, dx, dq, lane);
       }
-      D::tn(Ks, dx, dq, lane);
+      stage = then;
     }
   }
   if (q0 >= a.T) return;
@@ -508,6 +575,8 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
   RelKey key{0u, 0u};
   if (DROP) key = rel_key(a.rng, a.site);
   const unsigned short* map = BIAS ? a.by_key + (size_t)(u0 >> 5) * a.NT * 1024 : nullptr;
+  const Live live = live_start<BIAS>(reinterpret_cast<unsigned char*>(table + a.buckets + 1 + (a.buckets + 1 & 1)), a.live_key, BIAS ? *a.dead : 0, first >> 5, a.NT,
+                                     wave, lane);
   const int end = min(all, (group + 1) * units);
   int head = group * units / a.B, b = group * units - head * a.B;
   bool fresh = true;                 // the first image of its head here
@@ -520,91 +589,104 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
     if (BIAS && first_image) table_load(2 * STAGE, table, a, head, wave, waves, lane);
     float* sums = BIAS && pairs ? pairs + (((size_t)(group - rel_first_group(head, a.B, units)) * a.heads + head) * a.NT + (u0 >> 5)) * a.NT * 1024 + lane * 4 : nullptr;
     const T* base = qkv + (size_t)b * a.T * ld + head * DH;
-    const int tiles = first < n ? (n + 31) >> 5 : 0;
+    const int tiles = first < n ? (n + 31) >> 5 : 0, stages = (tiles + TS - 1) / TS;
+    auto tile_from = [&](int t) __attribute__((always_inline)) { return live_next(live.w, live.some, t, tiles); };
+    auto stage_from = [&](int k) __attribute__((always_inline)) {
+      const int t = live_next(live.all, live.some, k * TS, tiles);
+      return t < tiles ? t / TS : stages;
+    };
+    const int stage0 = stage_from(0);
     const bool mine = u0 < n;
     f32x16_t dk[D::NM], dv[D::NM];
 #pragma unroll
     for (int mt = 0; mt < D::NM; ++mt) dk[mt] = dv[mt] = zero16();
-    if (tiles) {
+    if (stage0 < stages) {
       Stager<T, DH> st;
       st.init(base, d_o + (size_t)b * a.T * d + head * DH, (unsigned)(ld * sizeof(T)), (unsigned)(d * sizeof(T)), n, lane);
       const i32x4_t rs = make_desc(rows + (size_t)bh * 3 * a.Tp, (unsigned)a.Tp * 12u);
-      auto load = [&](int s) __attribute__((always_inline)) {
-        const unsigned to = (s & 1) * STAGE;
+      auto load = [&](int s, int buf) __attribute__((always_inline)) {
+        const unsigned to = buf * STAGE;
         st.load(s * D::KB, to, wave, waves);
         if (lane < D::KB) {
           for (int k = waves - 1 - wave; k < 3; k += waves) load4_to_lds(rs, to + D::STAGE + k * D::KB * 4, (unsigned)(k * a.Tp + s * D::KB + lane) * 4u);
         }
       };
-      load(0);
+      load(stage0, 0);
+      int tn = mine ? tile_from(0) : tiles;
       MapRegs mr, next;
-      if (BIAS && mine) map_load(next, map, 0, lane);
+      if (BIAS && tn < tiles) map_load(next, map, tn, lane);
       typename D::Own bk, bv;
       D::own(base + d, ld, u, n, h, bk);
       D::scale(bk);
       D::own(base + 2 * d, ld, u, n, h, bv);
-      for (int t = 0; t < tiles; ++t) {
-        const int stage = t / TS;
-        if (t % TS == 0) {
-          // The loads of this stage are followed by at least the four stores of each tile before where there are sums.
-          asm volatile("" ::: "memory");
-          if (t && sums && mine) wait_vm<4 * TS>();
-          else wait_vm<0>();
-          workgroup_barrier();
-          if (t + TS < tiles) load(stage + 1);
-        }
-        if (!mine) continue;
-        if (BIAS) {
-          mr = next;
-          if (t + 1 < tiles) map_load(next, map, t + 1, lane);
-        }
-        float4 was[4];
-        if (BIAS && sums) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k) was[k] = float4{0.f, 0.f, 0.f, 0.f};
-          if (!first_image) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) was[k] = *reinterpret_cast<const float4*>(sums + (size_t)t * 1024 + k * 256);
+      int stored = 0;                // tiles whose sums this wavefront has stored since it issued the loads that it waits for
+      for (int stage = stage0, buf = 0; stage < stages; buf ^= 1) {
+        // Each of those tiles has left four stores behind the loads.
+        asm volatile("" ::: "memory");
+        if (stored >= 2) wait_vm<8>();
+        else if (stored == 1) wait_vm<4>();
+        else wait_vm<0>();
+        stored = 0;
+        workgroup_barrier();
+        const int then = stage_from(stage + 1);
+        if (then < stages) load(then, buf ^ 1);
+        while (tn < min(tiles, (stage + 1) * TS)) {
+          const int t = tn;
+          tn = tile_from(t + 1);
+          if (BIAS) {
+            mr = next;
+            if (tn < tiles) map_load(next, map, tn, lane);
           }
-        }
-        const unsigned char *S = smem + (stage & 1) * STAGE, *Qs = S + t % TS * TILE, *Gs = Qs + D::MAT;
-        const float* R = reinterpret_cast<const float*>(S + D::STAGE) + t % TS * 32;
-        f32x16_t p = score_tile<T, DH, BIAS>(Qs, bk, table, mr, a.scale, lane);
-        f32x16_t dx = D::nt(Gs, bv, zero16(), lane);
-        unsigned word[8];
-        if (DROP) draws_by_key(word, t * 32, (unsigned)u >> 1, (unsigned)bh, key, lane);
-  #pragma unroll
-        for (int i4 = 0; i4 < 4; ++i4) {
-          const float* r = R + i4 * 8 + h * 4;
-          const float4 m4 = *reinterpret_cast<const float4*>(r), l4 = *reinterpret_cast<const float4*>(r + D::KB), d4 = *reinterpret_cast<const float4*>(r + 2 * D::KB);
-          const float mm[4] = {m4.x, m4.y, m4.z, m4.w}, ll[4] = {l4.x, l4.y, l4.z, l4.w}, dd[4] = {d4.x, d4.y, d4.z, d4.w};
+          float4 was[4];
+          if (BIAS && sums) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int i = i4 * 4 + k;
-            const float pp = __builtin_amdgcn_exp2f(fmaf(p[i] - mm[k], kLog2e, -ll[k]));
-            if (DROP) {
-              const bool gone = draw_of(word, i) < a.dr.q;
-              p[i] = gone ? 0.f : pp;
-              dx[i] = pp * fmaf(dx[i], gone ? 0.f : a.dr.scale, -dd[k]);
-            } else {
-              p[i] = pp;
-              dx[i] = pp * (dx[i] - dd[k]);
+            for (int k = 0; k < 4; ++k) was[k] = float4{0.f, 0.f, 0.f, 0.f};
+            if (!first_image) {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) was[k] = *reinterpret_cast<const float4*>(sums + (size_t)t * 1024 + k * 256);
             }
           }
-        }
-        if (BIAS && sums) {
-          if (u0 + 32 > n) {       // keys past the image's tokens: probabilities that may be infinite
-            only_here();
+          const unsigned char *S = smem + buf * STAGE, *Qs = S + (t - stage * TS) * TILE, *Gs = Qs + D::MAT;
+          const float* R = reinterpret_cast<const float*>(S + D::STAGE) + (t - stage * TS) * 32;
+          f32x16_t p = score_tile<T, DH, BIAS>(Qs, bk, table, mr, a.scale, lane);
+          f32x16_t dx = D::nt(Gs, bv, zero16(), lane);
+          unsigned word[8];
+          if (DROP) draws_by_key(word, t * 32, (unsigned)u >> 1, (unsigned)bh, key, lane);
+    #pragma unroll
+          for (int i4 = 0; i4 < 4; ++i4) {
+            const float* r = R + i4 * 8 + h * 4;
+            const float4 m4 = *reinterpret_cast<const float4*>(r), l4 = *reinterpret_cast<const float4*>(r + D::KB), d4 = *reinterpret_cast<const float4*>(r + 2 * D::KB);
+            const float mm[4] = {m4.x, m4.y, m4.z, m4.w}, ll[4] = {l4.x, l4.y, l4.z, l4.w}, dd[4] = {d4.x, d4.y, d4.z, d4.w};
 #pragma unroll
-            for (int i = 0; i < 16; ++i) dx[i] = u < n ? dx[i] : 0.f;
+            for (int k = 0; k < 4; ++k) {
+              const int i = i4 * 4 + k;
+              const float pp = __builtin_amdgcn_exp2f(fmaf(p[i] - mm[k], kLog2e, -ll[k]));
+              if (DROP) {
+                const bool gone = draw_of(word, i) < a.dr.q;
+                p[i] = gone ? 0.f : pp;
+                dx[i] = pp * fmaf(dx[i], gone ? 0.f : a.dr.scale, -dd[k]);
+              } else {
+                p[i] = pp;
+                dx[i] = pp * (dx[i] - dd[k]);
+              }
+            }
           }
+          if (BIAS && sums) {
+            if (u0 + 32 > n) {       // keys past the image's tokens: probabilities that may be infinite
+              only_here();
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            *reinterpret_cast<float4*>(sums + (size_t)t * 1024 + k * 256) =
-                float4{was[k].x + dx[4 * k], was[k].y + dx[4 * k + 1], was[k].z + dx[4 * k + 2], was[k].w + dx[4 * k + 3]};
+              for (int i = 0; i < 16; ++i) dx[i] = u < n ? dx[i] : 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              *reinterpret_cast<float4*>(sums + (size_t)t * 1024 + k * 256) =
+                  float4{was[k].x + dx[4 * k], was[k].y + dx[4 * k + 1], was[k].z + dx[4 * k + 2], was[k].w + dx[4 * k + 3]};
+            ++stored;
+          }
+          D::tn(Gs, p, dv, lane);
+          D::tn(Qs, dx, dk, lane);
         }
-        D::tn(Gs, p, dv, lane);
-        D::tn(Qs, dx, dk, lane);
+        stage = then;
       }
     }
     if (u0 >= a.T) continue;
@@ -631,7 +713,7 @@ template <typename Kern> int allow_lds(Kern kern, size_t bytes) {      // more t
   if (bytes <= 65536) return CNNK_OK;
   return hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess ? CNNK_OK : CNNK_ERR_HIP;
 }
-size_t table_bytes(const RelArgs& a) { return a.buckets ? (size_t)(a.buckets + 1) * 4 : 0; }
+size_t table_bytes(const RelArgs& a) { return a.buckets ? (size_t)(a.buckets + 2) / 2 * 8 + kLiveBytes : 0; }      // and what is behind it
 
 // A workgroup's wavefronts: eight where the table takes so much LDS that a CU holds one workgroup (and the registers are there), otherwise four.
 int waves_of(const RelArgs& a, size_t lds, bool eight) {

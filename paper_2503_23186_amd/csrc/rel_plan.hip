@@ -19,7 +19,8 @@ __global__ void __launch_bounds__(256) buckets_grid_kernel(int gw, int gh, int c
 }
 
 __global__ void __launch_bounds__(256) plan_maps_kernel(int T, int NT, int buckets, const int* __restrict__ bucket, unsigned short* __restrict__ by_query,
-                                                        unsigned short* __restrict__ by_key) {
+                                                        unsigned short* __restrict__ by_key, int* __restrict__ dead) {
+  if (blockIdx.x == 0 && threadIdx.x == 0) *dead = 0;
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < (size_t)NT * NT * 1024; i += (size_t)gridDim.x * 256) {
     const int block = (int)(i >> 10), t = block / NT * 32 + (int)(i >> 5 & 31), u = block % NT * 32 + (int)(i & 31);
     int k = buckets;
@@ -29,6 +30,30 @@ __global__ void __launch_bounds__(256) plan_maps_kernel(int T, int NT, int bucke
     }
     by_query[((size_t)(t >> 5) * NT + (u >> 5)) * 1024 + rel_place(u & 31, t & 31)] = (unsigned short)(4 * k);
     by_key[((size_t)(u >> 5) * NT + (t >> 5)) * 1024 + rel_place(t & 31, u & 31)] = (unsigned short)(4 * k);
+  }
+}
+
+// A workgroup to a block of queries (blockIdx.y 0) or keys (1): which blocks of the others it has pairs with that are not masked
+__global__ void __launch_bounds__(256) plan_live_kernel(int NT, int buckets, const unsigned short* __restrict__ by_query, const unsigned short* __restrict__ by_key,
+                                                        unsigned long long* __restrict__ live_query, unsigned long long* __restrict__ live_key,
+                                                        int* __restrict__ dead) {
+  __shared__ unsigned any[256];
+  const unsigned short* map = (blockIdx.y ? by_key : by_query) + (size_t)blockIdx.x * NT * 1024;
+  any[threadIdx.x] = 0;
+  __syncthreads();
+  const int lane = threadIdx.x & 63;
+  for (int k = threadIdx.x >> 6; k < NT; k += 4) {
+    bool seen = false;
+    for (int i = 0; i < 16; ++i) seen |= map[(size_t)k * 1024 + i * 64 + lane] != 4 * buckets;
+    if (__any(seen) && lane == 0) any[k] = 1;
+  }
+  __syncthreads();
+  if (threadIdx.x < 4) {
+    unsigned long long m = 0;
+    for (int k = 0; k < 64; ++k) m |= (unsigned long long)any[threadIdx.x * 64 + k] << k;
+    (blockIdx.y ? live_key : live_query)[(size_t)blockIdx.x * 4 + threadIdx.x] = m;
+    const int here = min(64, max(0, NT - 64 * (int)threadIdx.x)) - __popcll(m);
+    if (blockIdx.y == 0 && here) atomicAdd(dead, here);
   }
 }
 
@@ -194,7 +219,10 @@ extern "C" int cnnk_rel_plan(int T, int buckets, const int* bucket, void* plan, 
   int *count = (int*)((char*)ws + runs_bytes(T)), *start = (int*)(p + at.start), *list = (int*)(p + at.list);
   const int NT = (T + 31) / 32, places = NT * NT * 1024, per = ((places + kParts - 1) / kParts + 63) / 64 * 64;
   const size_t lds = (size_t)buckets * 4, blocks = ((size_t)places + 255) / 256;
-  plan_maps_kernel<<<(unsigned)(blocks < 16384 ? blocks : 16384), 256, 0, st>>>(T, NT, buckets, bucket, (unsigned short*)(p + at.by_query), (unsigned short*)(p + at.by_key));
+  plan_maps_kernel<<<(unsigned)(blocks < 16384 ? blocks : 16384), 256, 0, st>>>(T, NT, buckets, bucket, (unsigned short*)(p + at.by_query), (unsigned short*)(p + at.by_key),
+                                                                                       (int*)(p + at.dead));
+  plan_live_kernel<<<dim3(NT, 2), 256, 0, st>>>(NT, buckets, (const unsigned short*)(p + at.by_query), (const unsigned short*)(p + at.by_key),
+                                               (unsigned long long*)(p + at.live_query), (unsigned long long*)(p + at.live_key), (int*)(p + at.dead));
   plan_order_kernel<<<NT * NT, 256, 0, st>>>(T, NT, buckets, bucket, (unsigned short*)(p + at.order), (unsigned*)(p + at.ends), runs);
   plan_count_kernel<<<kParts, 256, lds, st>>>(places, per, buckets, runs, count);
   plan_parts_kernel<<<(buckets + 255) / 256, 256, 0, st>>>(buckets, count, start);

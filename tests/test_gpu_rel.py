@@ -141,7 +141,10 @@ def test_grid_buckets(K, gh, gw, cls):
 
 def test_plans_are_reproducible_and_ignore_what_they_overwrite(K):
     T, n = 197, 30
-    m = torch.from_numpy(np.random.default_rng(1).integers(-2, n + 2, (T, T)).astype(np.int32)).to(DEV)
+    m = np.random.default_rng(1).integers(-2, n + 2, (T, T)).astype(np.int32)
+    m[64:96, 30:140] = -1
+    m[100:, 160:192] = n
+    m = torch.from_numpy(m).to(DEV)
     a = torch.full((K.cnnk_rel_plan_bytes(T, n),), 255, dtype=torch.uint8, device=DEV)
     b = torch.zeros_like(a)
     for p, fill in ((a, 255), (b, 0)):
@@ -164,8 +167,17 @@ def test_plans_are_reproducible_and_ignore_what_they_overwrite(K):
     # every pair of a bucket is in just one run, every run in the list of its bucket, in the order of the blocks
     order = part(a, 2 * size * 2, size, np.uint16).reshape(NT * NT, 64, 16) // 4
     ends = part(a, 3 * size * 2, NT * NT * 64, np.uint32).reshape(NT * NT, 64)
-    start = part(a, 3 * size * 2 + NT * NT * 256, n + 1, np.int32)
-    at = 3 * size * 2 + NT * NT * 256 + (4 * (n + 1) + 255) // 256 * 256
+    at = 3 * size * 2 + NT * NT * 256
+    live = part(a, at, NT * 8, np.uint64).reshape(2, NT, 4)
+    blocks = (padded < n).reshape(NT, 32, NT, 32).any((1, 3))    # queries, keys
+    for k, want in enumerate((blocks, blocks.T)):
+        got = live[k][:, np.arange(NT) // 64] >> (np.arange(NT) % 64).astype(np.uint64) & np.uint64(1)
+        assert (got == want).all()
+    at += (NT * 64 + 255) // 256 * 256
+    assert part(a, at, 1, np.int32)[0] == (~blocks).sum() > 0
+    at += 256
+    start = part(a, at, n + 1, np.int32)
+    at += (4 * (n + 1) + 255) // 256 * 256
     lists = [part(x, at, int(start[-1]), np.int32) for x in (a, b)]
     assert (lists[0] == lists[1]).all() and torch.equal(a[:3 * size * 2], b[:3 * size * 2])
     where = np.full(size, -1)                                    # bucket of the run at a place
@@ -291,6 +303,27 @@ def test_padded_batches(K, dtype, kind, p, T, heads, dh, lens):
     """What lies past an image's tokens is of no account: not a number there."""
     bucket, n = map_of(kind, T)
     Case(K, dtype, len(lens), T, heads, dh, bucket, n, p, lens=lens, past=np.nan).check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("p,lens", [(0.0, None), (0.2, [576, 300, 33])])
+@pytest.mark.parametrize("window,dh,heads", [(1, 64, 2), (3, 32, 1), (2, 128, 1), (5, 16, 2)])
+def test_windows(K, dtype, p, lens, window, dh, heads):
+    """Blocks of pairs that are masked as a whole are left out; among them those of 32 tokens that see nothing and those that nothing sees."""
+    side = 24
+    m = R.grid_buckets(side, side, 0)
+    y, x = np.arange(side * side) // side, np.arange(side * side) % side
+    m = np.where((np.abs(y[:, None] - y) > window) | (np.abs(x[:, None] - x) > window), -1, m)
+    m[64:96] = -1
+    m[:, 320:352] = 1 << 20
+    Case(K, dtype, 3 if lens else 1, side * side, heads, dh, m, (2 * side - 1) ** 2, p, lens=lens, past=np.nan).check()
+
+
+def test_a_map_that_masks_everything(K):
+    for T in (5, 70, 300):
+        c = Case(K, "bf16", 2, T, 2, 64, np.full((T, T), -1), 3, 0.3)
+        o, m, dq, dt = c.check()
+        assert (o == 0).all() and (dq == 0).all() and (dt == 0).all()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
