@@ -2,8 +2,14 @@
 #pragma once
 #include "rel.h"
 
+static inline FastDiv fast_div(unsigned d) {
+  FastDiv f;
+  f.init(d);
+  return f;
+}
 struct RelArgs {
   int B, T, Tp, heads, dh, NT, buckets;      // Tp: T rounded up to 64, NT: blocks of 32
+  FastDiv by_heads, by_images;
   float scale;                               // 1 / sqrt(dh)
   float down, up;                            // log2 of what probabilities are divided by while they are summed, and 2^down
   unsigned site;

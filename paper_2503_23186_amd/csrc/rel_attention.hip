@@ -96,6 +96,8 @@ RelArgs args_of(const cnnk_rel_desc* d, RelDrop dr, const float* table, const vo
   a.T = d->T;
   a.Tp = (d->T + 63) / 64 * 64;
   a.heads = d->heads;
+  a.by_heads = fast_div(d->heads);
+  a.by_images = fast_div(d->B);
   a.dh = d->dh;
   a.NT = (d->T + 31) / 32;
   a.buckets = d->buckets;

@@ -306,6 +306,14 @@ __device__ __forceinline__ void draws_by_key(unsigned (&word)[8], int query0, un
   }
 }
 
+// What a workgroup works on: which of `groups` (false: none) and which part of it.  The parts of one run on one XCD (every 8th workgroup shares its L2),
+// one behind the other.
+__device__ __forceinline__ bool group_part(int groups, FastDiv parts, int* group, int* part) {
+  int g;
+  parts.divmod((int)blockIdx.x >> 3, &g, part);
+  *group = g * 8 + (blockIdx.x & 7);
+  return *group < groups;
+}
 __device__ __forceinline__ float both_halves_max(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
@@ -316,19 +324,35 @@ __device__ __forceinline__ float both_halves_sum(float v) {
 }
 // Keeps the compiler from turning a branch that one tile of a walk takes into selects in every tile (a tenth of the forward pass).
 __device__ __forceinline__ void only_here() { asm volatile(""); }
+// times f, or 0 in lanes whose rows are not `there`; most wavefronts have all of them
+template <int N> __device__ __forceinline__ void scale_rows(f32x16_t* acc, float f, bool there) {
+  if (__all(there)) {
+    only_here();
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[k][i] *= f;
+  } else {
+    only_here();
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[k][i] = there ? acc[k][i] * f : 0.f;
+  }
+}
 __device__ __forceinline__ int key_of(int i, int h) { return (i >> 2) * 8 + h * 4 + (i & 3); }
 
 // ---- forward ---------------------------------------------------------------------------------------------------------------
 template <typename T, int DH, bool BIAS, bool DROP>
 __global__ void __launch_bounds__(512, sizeof(T) == 2 && DH <= 64 ? 4 : 2) rel_mfma_fwd_kernel(RelArgs a, const T* __restrict__ qkv, T* __restrict__ o,
-                                                                             float* __restrict__ stats, int parts) {
+                                                                             float* __restrict__ stats, FastDiv parts) {
   using D = Dim<T, DH>;
   constexpr int TS = D::KB / 32, TILE = D::PLANE / TS;      // tiles of a stage, bytes of a tile's rows in a plane
   extern __shared__ __align__(16) unsigned char smem[];
   int bh, part;
-  if (!head_part(a.B * a.heads, parts, &bh, &part)) return;
+  if (!group_part(a.B * a.heads, parts, &bh, &part)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = blockDim.x >> 6, h = lane >> 5;
-  const int b = bh / a.heads, head = bh - b * a.heads, d = a.heads * DH, n = rel_tokens(a, b);
+  const int b = a.by_heads.div(bh), head = bh - b * a.heads, d = a.heads * DH, n = rel_tokens(a, b);
   const size_t ld = 3 * (size_t)d;
   const int q0 = (part * waves + wave) * 32, q = q0 + (lane & 31), first = part * waves * 32;
   const T* base = qkv + (size_t)b * a.T * ld + head * DH;
@@ -421,11 +445,7 @@ __global__ void __launch_bounds__(512, sizeof(T) == 2 && DH <= 64 ? 4 : 2) rel_m
   if (q0 >= a.T) return;
   l = both_halves_sum(l);
   const bool any = q < n && l > 0.f;
-  const float inv = any ? a.dr.scale / l : 0.f;
-#pragma unroll
-  for (int mt = 0; mt < D::NM; ++mt)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) oacc[mt][i] = any ? oacc[mt][i] * inv : 0.f;
+  scale_rows<D::NM>(oacc, a.dr.scale / l, any);
   D::store(o + ((size_t)b * a.T + q) * d + head * DH, oacc, h, q < a.T);
   if (stats && h == 0 && q < a.T)
     *reinterpret_cast<float2*>(stats + ((size_t)bh * a.T + q) * 2) = any ? float2{m, kLn2 * __builtin_amdgcn_logf(l * a.up)} : float2{-INFINITY, 0.f};
@@ -437,14 +457,14 @@ __global__ void __launch_bounds__(512, sizeof(T) == 2 && DH <= 64 ? 4 : 2) rel_m
 template <typename T, int DH, bool BIAS, bool DROP>
 __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, sizeof(T) == 2 && DH <= 64 ? 3 : DH <= 64 ? 2 : 1) rel_mfma_dq_kernel(RelArgs a, const T* __restrict__ qkv, const T* __restrict__ o,
                                                                             const T* __restrict__ d_o, const float* __restrict__ stats,
-                                                                            T* __restrict__ dqkv, float* __restrict__ rows, int parts) {
+                                                                            T* __restrict__ dqkv, float* __restrict__ rows, FastDiv parts) {
   using D = Dim<T, DH>;
   constexpr int TS = D::KB / 32, TILE = D::PLANE / TS;      // tiles of a stage, bytes of a tile's rows in a plane
   extern __shared__ __align__(16) unsigned char smem[];
   int bh, part;
-  if (!head_part(a.B * a.heads, parts, &bh, &part)) return;
+  if (!group_part(a.B * a.heads, parts, &bh, &part)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = blockDim.x >> 6, h = lane >> 5;
-  const int b = bh / a.heads, head = bh - b * a.heads, d = a.heads * DH, n = rel_tokens(a, b);
+  const int b = a.by_heads.div(bh), head = bh - b * a.heads, d = a.heads * DH, n = rel_tokens(a, b);
   const size_t ld = 3 * (size_t)d;
   const int q0 = (part * waves + wave) * 32, q = q0 + (lane & 31), first = part * waves * 32;
   const T* base = qkv + (size_t)b * a.T * ld + head * DH;
@@ -539,10 +559,7 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, sizeof(T) == 2 && DH <= 
   }
   if (q0 >= a.T) return;
   lack = both_halves_sum(lack);
-#pragma unroll
-  for (int mt = 0; mt < D::NM; ++mt)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) dq[mt][i] = q < n ? dq[mt][i] * a.scale : 0.f;
+  scale_rows<D::NM>(dq, a.scale, q < n);
   D::store(dqkv + (size_t)b * a.T * ld + head * DH + (size_t)q * ld, dq, h, q < a.T);
   if (h == 0) {
     float* r = rows + (size_t)bh * 3 * a.Tp + q;
@@ -559,15 +576,15 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, sizeof(T) == 2 && DH <= 
 // no atomics.
 template <typename T, int DH, bool BIAS, bool DROP>
 __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mfma_dkv_kernel(RelArgs a, const T* __restrict__ qkv, const T* __restrict__ d_o,
-                                                                             const float* __restrict__ rows, T* __restrict__ dqkv, float* pairs, int parts,
-                                                                             int units) {
+                                                                             const float* __restrict__ rows, T* __restrict__ dqkv, float* pairs, FastDiv parts,
+                                                                             int units, int groups) {
   using D = Dim<T, DH>;
   constexpr int TS = D::KB / 32, TILE = D::PLANE / TS;      // tiles of a stage, bytes of a tile's rows in a plane
   extern __shared__ __align__(16) unsigned char smem[];
   constexpr int STAGE = D::STAGE + 3 * D::KB * 4;
   int group, part;
   const int all = a.B * a.heads;
-  if (!head_part((all + units - 1) / units, parts, &group, &part)) return;
+  if (!group_part(groups, parts, &group, &part)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), waves = blockDim.x >> 6, h = lane >> 5, d = a.heads * DH;
   const size_t ld = 3 * (size_t)d;
   const int u0 = (part * waves + wave) * 32, u = u0 + (lane & 31), first = part * waves * 32;
@@ -578,7 +595,7 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
   const Live live = live_start<BIAS>(reinterpret_cast<unsigned char*>(table + a.buckets + 1 + (a.buckets + 1 & 1)), a.live_key, BIAS ? *a.dead : 0, first >> 5, a.NT,
                                      wave, lane);
   const int end = min(all, (group + 1) * units);
-  int head = group * units / a.B, b = group * units - head * a.B;
+  int head = a.by_images.div(group * units), b = group * units - head * a.B;
   bool fresh = true;                 // the first image of its head here
   for (int unit = group * units; unit < end; ++unit, ++b) {
     if (b == a.B) b = 0, ++head, fresh = true;
@@ -695,14 +712,8 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
 #pragma unroll
         for (int k = 0; k < 4; ++k) *reinterpret_cast<float4*>(sums + (size_t)t * 1024 + k * 256) = float4{0.f, 0.f, 0.f, 0.f};
     }
-    const float up = DROP ? a.dr.scale : 1.f;
-#pragma unroll
-    for (int mt = 0; mt < D::NM; ++mt)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        dk[mt][i] = u < n ? dk[mt][i] * a.scale : 0.f;
-        dv[mt][i] = u < n ? dv[mt][i] * up : 0.f;
-      }
+    scale_rows<D::NM>(dk, a.scale, u < n);
+    scale_rows<D::NM>(dv, a.dr.scale, u < n);
     T* out = dqkv + (size_t)b * a.T * ld + head * DH + d + (size_t)u * ld;
     D::store(out, dk, h, u < a.T);
     D::store(out + d, dv, h, u < a.T);
@@ -726,7 +737,7 @@ int fwd_launch(const RelArgs& a, const T* qkv, T* o, float* stats, hipStream_t s
   const int waves = waves_of(a, lds, true), parts = (a.NT + waves - 1) / waves, pairs = a.B * a.heads;
   const auto kern = rel_mfma_fwd_kernel<T, DH, BIAS, DROP>;
   if (allow_lds(kern, lds) != CNNK_OK) return CNNK_ERR_HIP;
-  kern<<<(pairs + 7) / 8 * 8 * parts, 64 * waves, lds, st>>>(a, qkv, o, stats, parts);
+  kern<<<(pairs + 7) / 8 * 8 * parts, 64 * waves, lds, st>>>(a, qkv, o, stats, fast_div(parts));
   return launch_status();
 }
 template <typename T, int DH, bool BIAS, bool DROP>
@@ -736,8 +747,8 @@ int bwd_launch(const RelArgs& a, const T* qkv, const T* o, const T* d_o, const f
   const auto dq = rel_mfma_dq_kernel<T, DH, BIAS, DROP>;
   const auto dkv = rel_mfma_dkv_kernel<T, DH, BIAS, DROP>;
   if (allow_lds(dq, lds) != CNNK_OK || allow_lds(dkv, lds_kv) != CNNK_OK) return CNNK_ERR_HIP;
-  dq<<<(heads + 7) / 8 * 8 * parts, 64 * waves, lds, st>>>(a, qkv, o, d_o, stats, dqkv, rows, parts);
-  dkv<<<((heads + units - 1) / units + 7) / 8 * 8 * parts, 64 * waves, lds_kv, st>>>(a, qkv, d_o, rows, dqkv, pairs, parts, units);
+  dq<<<(heads + 7) / 8 * 8 * parts, 64 * waves, lds, st>>>(a, qkv, o, d_o, stats, dqkv, rows, fast_div(parts));
+  dkv<<<((heads + units - 1) / units + 7) / 8 * 8 * parts, 64 * waves, lds_kv, st>>>(a, qkv, d_o, rows, dqkv, pairs, fast_div(parts), units, (heads + units - 1) / units);
   return launch_status();
 }
 template <typename T, int DH> int fwd_of(const RelArgs& a, const T* qkv, T* o, float* stats, hipStream_t st) {
