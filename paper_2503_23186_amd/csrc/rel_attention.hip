@@ -15,6 +15,7 @@ __global__ void __launch_bounds__(256) rel_runs_kernel(RelArgs a, float* pairs, 
   const uint4 o0 = op[0], o1 = op[1];
   const unsigned w[8] = {o0.x, o0.y, o0.z, o0.w, o1.x, o1.y, o1.z, o1.w}, ends = a.ends[(size_t)block * 64 + lane];
   if (!__any(ends & 0xffffu)) return;       // masked pairs only: no walk has been there
+  const int runs = __builtin_amdgcn_readlane((int)((ends >> 16) + __popc(ends & 0xffffu)), 63);
   const int h1 = min(a.heads, ((int)blockIdx.y + 1) * heads_of);
   for (int h = blockIdx.y * heads_of; h < h1; ++h) {
     float* m = pairs + ((size_t)h * blocks + block) * 1024;
@@ -37,7 +38,7 @@ __global__ void __launch_bounds__(256) rel_runs_kernel(RelArgs a, float* pairs, 
 #pragma unroll
     for (int e = 0; e < 16; ++e) v[e] = *reinterpret_cast<const float*>(reinterpret_cast<const char*>(mine) + (e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xffffu));
     __builtin_amdgcn_wave_barrier();
-    float* out = m + (ends >> 16);
+    float* out = mine + (ends >> 16);
     float run = 0.f;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
@@ -47,6 +48,9 @@ __global__ void __launch_bounds__(256) rel_runs_kernel(RelArgs a, float* pairs, 
         run = 0.f;
       }
     }
+    __builtin_amdgcn_wave_barrier();
+    for (int k = lane; k < runs; k += 64) m[k] = mine[k];      // together: with a store for each of the sixteen 4096 tokens, 12 heads took 260 us instead of 239
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
