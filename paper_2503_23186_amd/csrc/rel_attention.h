@@ -29,13 +29,38 @@ __device__ __forceinline__ int rel_tokens(const RelArgs& a, int b) {
   return n < 0 ? 0 : n > a.T ? a.T : n;
 }
 
+// A block's sums by runs of one bucket (the plan's order): four quads of a lane in, the runs' sums out, one behind the other in the wavefront's 4 KB of LDS;
+// returns their number.
+__device__ __forceinline__ int rel_block_runs(float* mine, const float4 (&s)[4], uint4 o0, uint4 o1, unsigned ends, int lane) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) *reinterpret_cast<float4*>(mine + k * 256 + lane * 4) = s[k];
+  __builtin_amdgcn_wave_barrier();      // the wavefront's own part of LDS, which it uses in order
+  const unsigned w[8] = {o0.x, o0.y, o0.z, o0.w, o1.x, o1.y, o1.z, o1.w};
+  float v[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) v[e] = *reinterpret_cast<const float*>(reinterpret_cast<const char*>(mine) + (e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xffffu));
+  __builtin_amdgcn_wave_barrier();
+  float* out = mine + (ends >> 16);
+  float run = 0.f;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    run += v[e];
+    if (ends >> e & 1) {
+      *out++ = run;
+      run = 0.f;
+    }
+  }
+  __builtin_amdgcn_wave_barrier();
+  return __builtin_amdgcn_readlane((int)((ends >> 16) + __popc(ends & 0xffffu)), 63);
+}
+
 // the first workgroup that has images of a head, and how many have them
 __host__ __device__ __forceinline__ int rel_first_group(int head, int B, int units) { return (int)((long long)head * B / units); }
 __host__ __device__ __forceinline__ int rel_groups(int head, int B, int units) {
   return (int)(((long long)head * B + B - 1) / units) - rel_first_group(head, B, units) + 1;
 }
 // rows: [B * heads][3][Tp] floats; pairs (NULL: no gradient of the table): [slots][heads][NT][NT][1024]; units: (head, image) pairs
-// that a workgroup of the walk for dk and dv has.  T: bf16_t or float
+// that a workgroup of the walk for dk and dv has; *runs: whether it has left runs instead of pairs.  T: bf16_t or float
 template <typename T> int rel_mfma_fwd(const RelArgs& a, const T* qkv, T* o, float* stats, hipStream_t st);
 template <typename T>
-int rel_mfma_bwd(const RelArgs& a, const T* qkv, const T* o, const T* d_o, const float* stats, T* dqkv, float* rows, float* pairs, int units, hipStream_t st);
+int rel_mfma_bwd(const RelArgs& a, const T* qkv, const T* o, const T* d_o, const float* stats, T* dqkv, float* rows, float* pairs, int units, bool* runs, hipStream_t st);

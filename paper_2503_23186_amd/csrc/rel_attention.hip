@@ -4,18 +4,16 @@
 
 namespace {
 // Sums of a block's pairs over the workgroups' slots, then of its runs of one bucket.  A wavefront to a block and `heads_of` heads; the block's sums go through LDS in the
-// plan's order, sixteen to a lane, and a lane's runs to the block's place in the first slot.  A grid's map leaves 100 to 200 runs of 1024 pairs, so that the
-// gather behind this moves that much less (4096 tokens, 12 heads: 695 us for a gather of all pairs).
+// plan's order, sixteen to a lane, and its runs to the block's place in the first slot.  A grid's map leaves 100 to 200 runs of 1024 pairs, so that the
+// gather behind this moves that much less (4096 tokens, 12 heads: 695 us for a gather of all pairs, 239 and 57 this way).
 __global__ void __launch_bounds__(256) rel_runs_kernel(RelArgs a, float* pairs, int units, int heads_of) {
   __shared__ __align__(16) float sm[4][1024];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, blocks = a.NT * a.NT, block = blockIdx.x * 4 + wave;
   if (block >= blocks) return;
-  float* mine = sm[wave];
   const uint4* op = reinterpret_cast<const uint4*>(a.order + (size_t)block * 1024 + lane * 16);
   const uint4 o0 = op[0], o1 = op[1];
-  const unsigned w[8] = {o0.x, o0.y, o0.z, o0.w, o1.x, o1.y, o1.z, o1.w}, ends = a.ends[(size_t)block * 64 + lane];
+  const unsigned ends = a.ends[(size_t)block * 64 + lane];
   if (!__any(ends & 0xffffu)) return;       // masked pairs only: no walk has been there
-  const int runs = __builtin_amdgcn_readlane((int)((ends >> 16) + __popc(ends & 0xffffu)), 63);
   const int h1 = min(a.heads, ((int)blockIdx.y + 1) * heads_of);
   for (int h = blockIdx.y * heads_of; h < h1; ++h) {
     float* m = pairs + ((size_t)h * blocks + block) * 1024;
@@ -31,25 +29,8 @@ __global__ void __launch_bounds__(256) rel_runs_kernel(RelArgs a, float* pairs, 
         s[k].x += v.x, s[k].y += v.y, s[k].z += v.z, s[k].w += v.w;
       }
     }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) *reinterpret_cast<float4*>(mine + k * 256 + lane * 4) = s[k];
-    __builtin_amdgcn_wave_barrier();      // the wavefront's own part of LDS, which it uses in order
-    float v[16];
-#pragma unroll
-    for (int e = 0; e < 16; ++e) v[e] = *reinterpret_cast<const float*>(reinterpret_cast<const char*>(mine) + (e & 1 ? w[e >> 1] >> 16 : w[e >> 1] & 0xffffu));
-    __builtin_amdgcn_wave_barrier();
-    float* out = mine + (ends >> 16);
-    float run = 0.f;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      run += v[e];
-      if (ends >> e & 1) {
-        *out++ = run;
-        run = 0.f;
-      }
-    }
-    __builtin_amdgcn_wave_barrier();
-    for (int k = lane; k < runs; k += 64) m[k] = mine[k];      // together: with a store for each of the sixteen 4096 tokens, 12 heads took 260 us instead of 239
+    const int runs = rel_block_runs(sm[wave], s, o0, o1, ends, lane);
+    for (int k = lane; k < runs; k += 64) m[k] = sm[wave][k];
     __builtin_amdgcn_wave_barrier();
   }
 }
@@ -186,12 +167,13 @@ extern "C" int cnnk_rel_attention_bwd(const cnnk_rel_desc* d, const void* qkv, c
   float *rows = (float*)ws, *pairs = d->buckets && dtable ? (float*)((char*)ws + rows_bytes(d)) : nullptr;
   hipStream_t st = (hipStream_t)stream;
   const int units = units_of(d);
+  bool runs = false;
   const int r = d->dtype == CNNK_BF16
-                    ? rel_mfma_bwd(a, (const bf16_t*)qkv, (const bf16_t*)o, (const bf16_t*)d_o, stats, (bf16_t*)dqkv, rows, pairs, units, st)
-                    : rel_mfma_bwd(a, (const float*)qkv, (const float*)o, (const float*)d_o, stats, (float*)dqkv, rows, pairs, units, st);
+                    ? rel_mfma_bwd(a, (const bf16_t*)qkv, (const bf16_t*)o, (const bf16_t*)d_o, stats, (bf16_t*)dqkv, rows, pairs, units, &runs, st)
+                    : rel_mfma_bwd(a, (const float*)qkv, (const float*)o, (const float*)d_o, stats, (float*)dqkv, rows, pairs, units, &runs, st);
   if (r != CNNK_OK || !pairs) return r;
   const int blocks = a.NT * a.NT, heads_of = (int)((long)blocks * d->heads >= 65536 ? 4 : 1);
-  rel_runs_kernel<<<dim3((blocks + 3) / 4, (d->heads + heads_of - 1) / heads_of), 256, 0, st>>>(a, pairs, units, heads_of);
+  if (!runs) rel_runs_kernel<<<dim3((blocks + 3) / 4, (d->heads + heads_of - 1) / heads_of), 256, 0, st>>>(a, pairs, units, heads_of);
   // enough threads to fill the device where buckets are few
   int lanes = 8;
   while (lanes < 256 && (long)d->buckets * d->heads * lanes < 131072) lanes *= 2;

@@ -574,10 +574,10 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, sizeof(T) == 2 && DH <= 
 // dx of its keys to pairs [slot][heads][NT keys][NT queries][4][64][4], the slot being the workgroup's number among those that have images of the head: a
 // tile's sums so far come in while its scores are formed; they are a wavefront's own, in the caches, so the sum over images has one order and needs
 // no atomics.
-template <typename T, int DH, bool BIAS, bool DROP>
+template <typename T, int DH, bool BIAS, bool DROP, bool RUNS>
 __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mfma_dkv_kernel(RelArgs a, const T* __restrict__ qkv, const T* __restrict__ d_o,
                                                                              const float* __restrict__ rows, T* __restrict__ dqkv, float* pairs, FastDiv parts,
-                                                                             int units, int groups) {
+                                                                             int units, int groups, unsigned own_lds) {
   using D = Dim<T, DH>;
   constexpr int TS = D::KB / 32, TILE = D::PLANE / TS;      // tiles of a stage, bytes of a tile's rows in a plane
   extern __shared__ __align__(16) unsigned char smem[];
@@ -589,6 +589,7 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
   const size_t ld = 3 * (size_t)d;
   const int u0 = (part * waves + wave) * 32, u = u0 + (lane & 31), first = part * waves * 32;
   float* table = reinterpret_cast<float*>(smem + 2 * STAGE);
+  float* block_lds = reinterpret_cast<float*>(smem + own_lds) + wave * 1024;      // RUNS: where a block becomes runs
   RelKey key{0u, 0u};
   if (DROP) key = rel_key(a.rng, a.site);
   const unsigned short* map = BIAS ? a.by_key + (size_t)(u0 >> 5) * a.NT * 1024 : nullptr;
@@ -655,7 +656,7 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
             if (tn < tiles) map_load(next, map, tn, lane);
           }
           float4 was[4];
-          if (BIAS && sums) {
+          if (BIAS && !RUNS && sums) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) was[k] = float4{0.f, 0.f, 0.f, 0.f};
             if (!first_image) {
@@ -694,11 +695,21 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
 #pragma unroll
               for (int i = 0; i < 16; ++i) dx[i] = u < n ? dx[i] : 0.f;
             }
+            if (!RUNS) {
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-              *reinterpret_cast<float4*>(sums + (size_t)t * 1024 + k * 256) =
-                  float4{was[k].x + dx[4 * k], was[k].y + dx[4 * k + 1], was[k].z + dx[4 * k + 2], was[k].w + dx[4 * k + 3]};
-            ++stored;
+              for (int k = 0; k < 4; ++k)
+                *reinterpret_cast<float4*>(sums + (size_t)t * 1024 + k * 256) =
+                    float4{was[k].x + dx[4 * k], was[k].y + dx[4 * k + 1], was[k].z + dx[4 * k + 2], was[k].w + dx[4 * k + 3]};
+              ++stored;
+            } else {
+              const size_t block = (size_t)(u0 >> 5) * a.NT + t;
+              const uint4* op = reinterpret_cast<const uint4*>(a.order + block * 1024 + lane * 16);
+              const float4 q[4] = {{dx[0], dx[1], dx[2], dx[3]}, {dx[4], dx[5], dx[6], dx[7]}, {dx[8], dx[9], dx[10], dx[11]}, {dx[12], dx[13], dx[14], dx[15]}};
+              const int runs = rel_block_runs(block_lds, q, op[0], op[1], a.ends[block * 64 + lane], lane);
+              float* m = sums - lane * 4 + (size_t)t * 1024;
+              for (int k = lane; k < runs; k += 64) m[k] = block_lds[k];
+              __builtin_amdgcn_wave_barrier();
+            }
           }
           D::tn(Gs, p, dv, lane);
           D::tn(Qs, dx, dk, lane);
@@ -724,7 +735,7 @@ template <typename Kern> int allow_lds(Kern kern, size_t bytes) {      // more t
   if (bytes <= 65536) return CNNK_OK;
   return hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess ? CNNK_OK : CNNK_ERR_HIP;
 }
-size_t table_bytes(const RelArgs& a) { return a.buckets ? (size_t)(a.buckets + 2) / 2 * 8 + kLiveBytes : 0; }      // and what is behind it
+size_t table_bytes(const RelArgs& a) { return a.buckets ? align_up((size_t)(a.buckets + 2) / 2 * 8 + kLiveBytes, 16) : 0; }      // and what is behind it
 
 // A workgroup's wavefronts: eight where the table takes so much LDS that a CU holds one workgroup (and the registers are there), otherwise four.
 int waves_of(const RelArgs& a, size_t lds, bool eight) {
@@ -741,14 +752,23 @@ int fwd_launch(const RelArgs& a, const T* qkv, T* o, float* stats, hipStream_t s
   return launch_status();
 }
 template <typename T, int DH, bool BIAS, bool DROP>
-int bwd_launch(const RelArgs& a, const T* qkv, const T* o, const T* d_o, const float* stats, T* dqkv, float* rows, float* pairs, int units, hipStream_t st) {
+int bwd_launch(const RelArgs& a, const T* qkv, const T* o, const T* d_o, const float* stats, T* dqkv, float* rows, float* pairs, int units, bool* runs, hipStream_t st) {
   const size_t lds = 2 * Dim<T, DH>::STAGE + table_bytes(a), lds_kv = lds + 2 * 3 * Dim<T, DH>::KB * 4;
   const int waves = waves_of(a, lds_kv, DH <= 64), parts = (a.NT + waves - 1) / waves, heads = a.B * a.heads;
+  // The walk itself adds up a block's runs (which makes it longer) where a single image's sums of pairs are more than the caches hold, so that a kernel behind it would
+  // read them from memory, and where the workgroup has a CU's LDS to itself.  us of the walk, the runs and the gather, 12 heads of 64 bf16, pairs written | runs written:
+  // 1024 tokens (a table for 4096) 84 | 101, 3136 tokens 401 | 357, 4096 tokens 619 | 462, 4096 tokens in windows of 15 x 15 150 | 150.  With more images it would
+  // have to be done in each: 8 x 1600 tokens 571 | 632, 4 x 4096 tokens 1749 | 1911.
+  *runs = pairs && a.B == 1 && waves == 8 && (size_t)a.heads * a.NT * a.NT * 4096 > (size_t)256 << 20;
+  const size_t lds_runs = *runs ? waves * 4096 : 0;
   const auto dq = rel_mfma_dq_kernel<T, DH, BIAS, DROP>;
-  const auto dkv = rel_mfma_dkv_kernel<T, DH, BIAS, DROP>;
-  if (allow_lds(dq, lds) != CNNK_OK || allow_lds(dkv, lds_kv) != CNNK_OK) return CNNK_ERR_HIP;
+  auto dkv = rel_mfma_dkv_kernel<T, DH, BIAS, DROP, false>;
+  if constexpr (BIAS && DH <= 64)
+    if (*runs) dkv = rel_mfma_dkv_kernel<T, DH, BIAS, DROP, true>;
+  if (allow_lds(dq, lds) != CNNK_OK || allow_lds(dkv, lds_kv + lds_runs) != CNNK_OK) return CNNK_ERR_HIP;
   dq<<<(heads + 7) / 8 * 8 * parts, 64 * waves, lds, st>>>(a, qkv, o, d_o, stats, dqkv, rows, fast_div(parts));
-  dkv<<<((heads + units - 1) / units + 7) / 8 * 8 * parts, 64 * waves, lds_kv, st>>>(a, qkv, d_o, rows, dqkv, pairs, fast_div(parts), units, (heads + units - 1) / units);
+  dkv<<<((heads + units - 1) / units + 7) / 8 * 8 * parts, 64 * waves, lds_kv + lds_runs, st>>>(a, qkv, d_o, rows, dqkv, pairs, fast_div(parts), units, (heads + units - 1) / units,
+                                                                                                               (unsigned)lds_kv);
   return launch_status();
 }
 template <typename T, int DH> int fwd_of(const RelArgs& a, const T* qkv, T* o, float* stats, hipStream_t st) {
@@ -756,12 +776,12 @@ template <typename T, int DH> int fwd_of(const RelArgs& a, const T* qkv, T* o, f
   return a.dr.q ? fwd_launch<T, DH, false, true>(a, qkv, o, stats, st) : fwd_launch<T, DH, false, false>(a, qkv, o, stats, st);
 }
 template <typename T, int DH>
-int bwd_of(const RelArgs& a, const T* qkv, const T* o, const T* d_o, const float* stats, T* dqkv, float* rows, float* pairs, int units, hipStream_t st) {
+int bwd_of(const RelArgs& a, const T* qkv, const T* o, const T* d_o, const float* stats, T* dqkv, float* rows, float* pairs, int units, bool* runs, hipStream_t st) {
   if (a.buckets)
-    return a.dr.q ? bwd_launch<T, DH, true, true>(a, qkv, o, d_o, stats, dqkv, rows, pairs, units, st)
-                  : bwd_launch<T, DH, true, false>(a, qkv, o, d_o, stats, dqkv, rows, pairs, units, st);
-  return a.dr.q ? bwd_launch<T, DH, false, true>(a, qkv, o, d_o, stats, dqkv, rows, pairs, units, st)
-                : bwd_launch<T, DH, false, false>(a, qkv, o, d_o, stats, dqkv, rows, pairs, units, st);
+    return a.dr.q ? bwd_launch<T, DH, true, true>(a, qkv, o, d_o, stats, dqkv, rows, pairs, units, runs, st)
+                  : bwd_launch<T, DH, true, false>(a, qkv, o, d_o, stats, dqkv, rows, pairs, units, runs, st);
+  return a.dr.q ? bwd_launch<T, DH, false, true>(a, qkv, o, d_o, stats, dqkv, rows, pairs, units, runs, st)
+                : bwd_launch<T, DH, false, false>(a, qkv, o, d_o, stats, dqkv, rows, pairs, units, runs, st);
 }
 }  // namespace
 
@@ -774,11 +794,11 @@ template <typename T> int rel_mfma_fwd(const RelArgs& a, const T* qkv, T* o, flo
   }
 }
 template <typename T>
-int rel_mfma_bwd(const RelArgs& a, const T* qkv, const T* o, const T* d_o, const float* stats, T* dqkv, float* rows, float* pairs, int units, hipStream_t st) {
+int rel_mfma_bwd(const RelArgs& a, const T* qkv, const T* o, const T* d_o, const float* stats, T* dqkv, float* rows, float* pairs, int units, bool* runs, hipStream_t st) {
   switch (a.dh) {
-    case 16: return bwd_of<T, 16>(a, qkv, o, d_o, stats, dqkv, rows, pairs, units, st);
-    case 32: return bwd_of<T, 32>(a, qkv, o, d_o, stats, dqkv, rows, pairs, units, st);
-    case 64: return bwd_of<T, 64>(a, qkv, o, d_o, stats, dqkv, rows, pairs, units, st);
-    default: return bwd_of<T, 128>(a, qkv, o, d_o, stats, dqkv, rows, pairs, units, st);
+    case 16: return bwd_of<T, 16>(a, qkv, o, d_o, stats, dqkv, rows, pairs, units, runs, st);
+    case 32: return bwd_of<T, 32>(a, qkv, o, d_o, stats, dqkv, rows, pairs, units, runs, st);
+    case 64: return bwd_of<T, 64>(a, qkv, o, d_o, stats, dqkv, rows, pairs, units, runs, st);
+    default: return bwd_of<T, 128>(a, qkv, o, d_o, stats, dqkv, rows, pairs, units, runs, st);
   }
 }

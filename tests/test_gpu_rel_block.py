@@ -216,3 +216,45 @@ def test_large_tables_and_long_sequences(K, dtype, T, heads, dh, buckets):
     assert off(o, wo) <= half and off(dq, wd) <= 2 * half
     if buckets:
         assert off(dt, wt) <= (T + 64) * 2.0 ** -24 + 2.0 ** -17
+
+
+@pytest.mark.parametrize("dtype,heads,dh,kind,lens,side", [
+    ("bf16", 8, 64, "grid", [700, 2080, 0, 1500], (40, 52)), ("bf16", 10, 32, "window", [2080, 31], (40, 52)), ("bf16", 17, 128, "grid", [2080], (40, 52)),
+    ("bf16", 8, 64, "grid", [3050], (50, 61)), ("f32", 8, 64, "grid", [2999], (50, 61)), ("bf16", 9, 64, "window", [3001], (48, 65)), ("f32", 8, 64, "random", [3001], (50, 61)),
+    ("bf16", 8, 64, "random", [0], (50, 61))])
+def test_long_padded_batches(K, dtype, heads, dh, kind, lens, side):
+    """Sums of dx of more than 256 MB, one image and several, images shorter than T."""
+    T, B, n = side[0] * side[1], len(lens), K.grid_buckets(*side, 0)
+    gen = torch.Generator(device=DEV).manual_seed(dh)
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    rand = lambda *s: torch.randn(*s, generator=gen, device=DEV)
+    qkv, g = rand(B, T, 3 * heads * dh).to(t), rand(B, T, heads * dh).to(t)
+    bucket = torch.empty(T, T, dtype=torch.int32, device=DEV)
+    st = torch.cuda.current_stream().cuda_stream
+    K.cnnk_rel_buckets_grid(*side, 0, bucket, st)
+    if kind == "window":
+        i = torch.arange(T, device=DEV)
+        bucket[((i[:, None] // side[1] - i[None] // side[1]).abs() > 4) | ((i[:, None] % side[1] - i[None] % side[1]).abs() > 4)] = -1
+    elif kind == "random":
+        bucket, n = torch.randint(-1, 12500, (T, T), generator=gen, device=DEV, dtype=torch.int32), 12500
+    table, plan = rand(n, heads), K.make_plan(bucket, n)
+    d = K.rel_desc(B, T, heads, dh, K.BF16 if dtype == "bf16" else K.F32, n, 0.0, 0)
+    gl = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    o, stats, dq, dt = torch.full_like(g, 7.0), torch.empty(B, heads, T, 2, device=DEV), torch.full_like(qkv, 7.0), torch.full_like(table, 7.0)
+    ws = torch.full((K.cnnk_rel_attention_workspace_bytes(d),), 255, dtype=torch.uint8, device=DEV)
+    K.cnnk_rel_attention_fwd(d, qkv, table, plan, gl, None, o, stats, st)
+    K.cnnk_rel_attention_bwd(d, qkv, o, g, table, plan, gl, None, stats, dq, dt, ws, ws.numel(), st)
+    off = lambda a, b: float((a.double() - b).norm() / b.norm())
+    half = 2.0 ** -8 if dtype == "bf16" else (T + 64) * 2.0 ** -24
+    total = torch.zeros_like(table, dtype=torch.float64)
+    for b, m in enumerate(lens):
+        assert (o[b, m:] == 0).all() and (dq[b, m:] == 0).all()
+        if m:
+            wo, wd, wt = reference64(qkv[b, :m].contiguous(), heads, dh, table, bucket[:m, :m].contiguous(), g[b, :m].contiguous())
+            assert off(o[b, :m], wo) <= half and off(dq[b, :m], wd) <= 2 * half
+            total += wt
+    assert off(dt, total) <= (T + 64) * 2.0 ** -24 + 2.0 ** -17 if max(lens) else (dt == 0).all()
+    again = torch.full_like(table, 3.0)
+    ws.fill_(1)
+    K.cnnk_rel_attention_bwd(d, qkv, o, g, table, plan, gl, None, stats, dq, again, ws, ws.numel(), st)
+    assert torch.equal(again, dt)
