@@ -45,10 +45,10 @@ __device__ __forceinline__ int rel_block_runs(float* mine, const float4 (&s)[4],
 #pragma unroll
   for (int e = 0; e < 16; ++e) {
     run += v[e];
-    if (ends >> e & 1) {
-      *out++ = run;
-      run = 0.f;
-    }
+    *out = run;       // over itself until the run ends: with a branch around the store the walk of 4096 tokens, 12 heads took 375 us instead of 349
+    const unsigned last = ends >> e & 1;
+    out += last;
+    run = last ? 0.f : run;
   }
   __builtin_amdgcn_wave_barrier();
   return __builtin_amdgcn_readlane((int)((ends >> 16) + __popc(ends & 0xffffu)), 63);

@@ -757,7 +757,7 @@ int bwd_launch(const RelArgs& a, const T* qkv, const T* o, const T* d_o, const f
   const int waves = waves_of(a, lds_kv, DH <= 64), parts = (a.NT + waves - 1) / waves, heads = a.B * a.heads;
   // The walk itself adds up a block's runs (which makes it longer) where a single image's sums of pairs are more than the caches hold, so that a kernel behind it would
   // read them from memory, and where the workgroup has a CU's LDS to itself.  us of the walk, the runs and the gather, 12 heads of 64 bf16, pairs written | runs written:
-  // 1024 tokens (a table for 4096) 84 | 101, 3136 tokens 401 | 357, 4096 tokens 619 | 462, 4096 tokens in windows of 15 x 15 150 | 150.  With more images it would
+  // 1024 tokens (a table for 4096) 84 | 101, 3136 tokens 401 | 340, 4096 tokens 619 | 436, 4096 tokens in windows of 15 x 15 150 | 143.  With more images it would
   // have to be done in each: 8 x 1600 tokens 571 | 632, 4 x 4096 tokens 1749 | 1911.
   *runs = pairs && a.B == 1 && waves == 8 && (size_t)a.heads * a.NT * a.NT * 4096 > (size_t)256 << 20;
   const size_t lds_runs = *runs ? waves * 4096 : 0;
