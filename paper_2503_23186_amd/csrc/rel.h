@@ -35,12 +35,13 @@ __device__ __forceinline__ RelKey rel_key(const unsigned long long* rng, unsigne
 constexpr unsigned kDrawElements = 0, kDrawGroups = 1, kDrawPairs = 2;      // last word of the counter
 
 // p as a call takes it: elements whose 16-bit draw is below q are dropped, the others scaled by `scale`
-struct RelDrop { unsigned q; float scale; };
+struct RelDrop { unsigned q; float scale, keep; };      // keep: 1 / scale, exactly
 static inline int rel_drop(float p, RelDrop* out) {
   if (!(p >= 0.f && p < 1.f)) return CNNK_ERR_SHAPE;
   out->q = (unsigned)((double)p * 65536.0 + 0.5);
   if (out->q >= 65536u) return CNNK_ERR_UNSUPPORTED;
   out->scale = (float)(65536.0 / (65536.0 - out->q));
+  out->keep = (float)(65536 - out->q) / 65536.f;
   return CNNK_OK;
 }
 

@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(256) rel_buckets_kernel(RelArgs a, const float
     __syncthreads();
     if (j < w) sm[threadIdx.x] += sm[threadIdx.x + w];
   }
-  if (j == 0 && k < a.buckets) dtable[(size_t)k * a.heads + h] = sm[threadIdx.x];
+  if (j == 0 && k < a.buckets) dtable[(size_t)k * a.heads + h] = sm[threadIdx.x] * a.dr.scale;
 }
 
 int check(const cnnk_rel_desc* d, RelDrop* dr) {

@@ -14,7 +14,8 @@
 //
 // dx = P (dP - delta) with delta = sum P dP.  do . o is delta up to what rounding took off o and off the probabilities in front of it (2^-7 of its terms),
 // which is as exact as dq's own operands are but would show in the table's gradient, an fp32 sum.  The walk for dq takes it as an estimate; its
-// dx' = P (dP - estimate) sum to what the estimate lacks, so that the walk behind it has delta to fp32.
+// dx' = P (dP - estimate) sum to what the estimate lacks, so that the walk behind it has delta to fp32.  With dropout both walks, and the sums for the table, have
+// dx divided by the kept values' factor, so that dP and delta cancel in rows with a single pair without the rounding of a product.
 //
 // Dropout: a call of the generator gives eight draws, of four queries and two keys (include/cnnk_rel.h).  With a query a lane, four neighbouring
 // lanes need the four words of the same calls: each makes a quarter of the calls and they transpose words among
@@ -144,6 +145,23 @@ template <int DH> struct Dim<float, DH> {
       }
   }
 };
+
+// acc += M^T x in the backward pass.  bf16: x is rounded to 2^-8, as is the result.  Over many pairs that is one more rounding of the result's own size (1.43 times its error
+// alone); with a few tokens it is up to 1.56 times, so images of one tile add a product with what the rounding took off (1.05 to 1.3
+// times; both walks together 21.8 -> 23.0 us at 64 images of 25 tokens and 12 heads of 64, where starting takes most of it).
+template <typename T, int DH> __device__ __forceinline__ void tn_bwd(const unsigned char* m, const f32x16_t& x, f32x16_t* acc, int lane, bool one_tile) {
+  Dim<T, DH>::tn(m, x, acc, lane);
+  if (sizeof(T) == 2 && one_tile) {
+    f32x16_t r;
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+      const unsigned w = pack_bf16x2(x[i], x[i + 1]);
+      r[i] = x[i] - __uint_as_float(w << 16);
+      r[i + 1] = x[i + 1] - __uint_as_float(w & 0xffff0000u);
+    }
+    Dim<T, DH>::tn(m, r, acc, lane);
+  }
+}
 
 // ---- stages: KB rows of two matrices -----------------------------------------------------------------------------------------
 // A wavefront's direct load fills LOAD_ROWS rows of a plane, 1 KB.
@@ -496,7 +514,7 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, sizeof(T) == 2 && DH <= 
     {
       typename D::Own t;
       D::own(o + head0, d, q, n, h, t);
-      delta = both_halves_sum(D::dot(t, bg));
+      delta = both_halves_sum(D::dot(t, bg)) * a.dr.keep;
     }
     if (q < n) {
       const float2 s = *reinterpret_cast<const float2*>(stats + ((size_t)bh * a.T + q) * 2);
@@ -536,9 +554,8 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, sizeof(T) == 2 && DH <= 
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           p[i] = __builtin_amdgcn_exp2f(fmaf(p[i] - m, kLog2e, -L2));
-          float w = 1.f;
-          if (DROP) w = draw_of(word, i) < a.dr.q ? 0.f : a.dr.scale;
-          dx[i] = p[i] * (DROP ? fmaf(dx[i], w, -delta) : dx[i] - delta);
+          if (DROP) dx[i] = draw_of(word, i) < a.dr.q ? 0.f : dx[i];
+          dx[i] = p[i] * (dx[i] - delta);
         }
         if (t * 32 + 32 > n) {       // keys past the image's tokens: rows of zeros, whose probabilities may be infinite
           only_here();
@@ -552,14 +569,14 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, sizeof(T) == 2 && DH <= 
           for (int i = 0; i < 16; ++i) add[i & 1] += dx[i];
           lack += add[0] + add[1];
         }
-        D::tn(Ks, dx, dq, lane);
+        tn_bwd<T, DH>(Ks, dx, dq, lane, a.NT == 1);
       }
       stage = then;
     }
   }
   if (q0 >= a.T) return;
   lack = both_halves_sum(lack);
-  scale_rows<D::NM>(dq, a.scale, q < n);
+  scale_rows<D::NM>(dq, a.scale * a.dr.scale, q < n);
   D::store(dqkv + (size_t)b * a.T * ld + head * DH + (size_t)q * ld, dq, h, q < a.T);
   if (h == 0) {
     float* r = rows + (size_t)bh * 3 * a.Tp + q;
@@ -682,7 +699,7 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
               if (DROP) {
                 const bool gone = draw_of(word, i) < a.dr.q;
                 p[i] = gone ? 0.f : pp;
-                dx[i] = pp * fmaf(dx[i], gone ? 0.f : a.dr.scale, -dd[k]);
+                dx[i] = pp * ((gone ? 0.f : dx[i]) - dd[k]);
               } else {
                 p[i] = pp;
                 dx[i] = pp * (dx[i] - dd[k]);
@@ -711,8 +728,8 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
               __builtin_amdgcn_wave_barrier();
             }
           }
-          D::tn(Gs, p, dv, lane);
-          D::tn(Qs, dx, dk, lane);
+          tn_bwd<T, DH>(Gs, p, dv, lane, a.NT == 1);
+          tn_bwd<T, DH>(Qs, dx, dk, lane, a.NT == 1);
         }
         stage = then;
       }
@@ -723,7 +740,7 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
 #pragma unroll
         for (int k = 0; k < 4; ++k) *reinterpret_cast<float4*>(sums + (size_t)t * 1024 + k * 256) = float4{0.f, 0.f, 0.f, 0.f};
     }
-    scale_rows<D::NM>(dk, a.scale, u < n);
+    scale_rows<D::NM>(dk, a.scale * a.dr.scale, u < n);
     scale_rows<D::NM>(dv, a.dr.scale, u < n);
     T* out = dqkv + (size_t)b * a.T * ld + head * DH + d + (size_t)u * ld;
     D::store(out, dk, h, u < a.T);

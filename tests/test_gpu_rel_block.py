@@ -258,3 +258,42 @@ def test_long_padded_batches(K, dtype, heads, dh, kind, lens, side):
     ws.fill_(1)
     K.cnnk_rel_attention_bwd(d, qkv, o, g, table, plan, gl, None, stats, dq, again, ws, ws.numel(), st)
     assert torch.equal(again, dt)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("p", [0.0, 0.2])
+def test_a_row_with_one_key_gives_no_gradient_to_scores(K, dtype, p):
+    """The softmax of one score is 1 whatever the score is: dq, dk and dtable are zero, and dv is what the kept values' factor makes of d_o.
+
+    dx = dP - delta: both are sums of dh products, (dh + 8) 2^-24 of the sum S of their magnitudes each; delta's estimate, which dq is made of, is off by o's rounding besides."""
+    B, T, heads, dh, n = 5, 37, 3, 64, 8
+    gen = torch.Generator(device=DEV).manual_seed(4)
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    qkv, g = torch.randn(B, T, 3 * heads * dh, generator=gen, device=DEV).to(t), torch.randn(B, T, heads * dh, generator=gen, device=DEV).to(t)
+    bucket = torch.full((T, T), -1, dtype=torch.int32, device=DEV)
+    key = torch.randperm(T, generator=gen, device=DEV)
+    bucket[torch.arange(T, device=DEV), key] = (key % n).int()
+    table, plan = torch.randn(n, heads, generator=gen, device=DEV), K.make_plan(bucket, n)
+    d = K.rel_desc(B, T, heads, dh, K.BF16 if dtype == "bf16" else K.F32, n, p, 3)
+    rng = torch.tensor([7, 1], dtype=torch.int64, device=DEV)
+    st = torch.cuda.current_stream().cuda_stream
+    o, stats, dq, dt = torch.empty_like(g), torch.empty(B, heads, T, 2, device=DEV), torch.empty_like(qkv), torch.empty_like(table)
+    ws = torch.empty(K.cnnk_rel_attention_workspace_bytes(d), dtype=torch.uint8, device=DEV)
+    K.cnnk_rel_attention_fwd(d, qkv, table, plan, None, rng, o, stats, st)
+    K.cnnk_rel_attention_bwd(d, qkv, o, g, table, plan, None, rng, stats, dq, dt, ws, ws.numel(), st)
+    dim = heads * dh
+    v = qkv[:, key, 2 * dim:].float()
+    kept = (o.float() / v).view(B, T, heads, dh)[..., 0].round()      # 0 or 1 (the factor is below 1.5)
+    factor = 65536 / (65536 - round(65536 * p))
+    assert p == 0 or 0 < kept.mean() < 1
+    split = lambda x: x.double().view(B, T, heads, dh)
+    S = (split(g) * split(v)).abs().sum(-1, keepdim=True) * factor
+    sums, rounding = 2 * (dh + 8) * 2.0 ** -24, 2.0 ** -8 if dtype == "bf16" else 2.0 ** -23
+    scale = 1.01 / dh ** 0.5
+    assert (split(dq[..., :dim]).abs() <= S * (sums + rounding) * split(qkv[:, key, dim:2 * dim]).abs() * scale).all()
+    assert (split(dq[:, key, dim:2 * dim]).abs() <= S * sums * split(qkv[..., :dim]).abs() * scale).all()
+    dx = torch.zeros(n, heads, dtype=torch.float64, device=DEV).index_add_(0, key % n, S.sum(0)[..., 0] * sums)
+    assert (dt.double().abs() <= dx * 1.01).all()
+    want = torch.zeros_like(g, dtype=torch.float32)
+    want[:, key] = (g.float().view(B, T, heads, dh) * (kept * factor)[..., None]).view(B, T, dim)
+    assert ((dq[..., 2 * dim:].float() - want).abs() <= want.abs() * (2.0 ** -8 if dtype == "bf16" else 2.0 ** -21) * 1.01).all()
