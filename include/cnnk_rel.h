@@ -71,13 +71,14 @@ int cnnk_rel_plan(int T, int buckets, const int* bucket, void* plan, void* ws, s
  * Training: stats [B][heads][T][2] receives a reference near each row's largest x and the logarithm of
  * sum_u exp(x - reference) (a row that sees no key: -infinity and 0);
  * NULL in evaluation.
- * dh in {16, 32, 64, 128}; T <= 16384, 8192 with buckets; heads <= 65535; the elements of an image's qkv take less than 2^31 bytes. */
+ * dh in {16, 32, 64, 128}; T <= 16384, 8192 with buckets; heads <= 65535; the elements of an image's qkv take less than 2^31 bytes;
+ * (B * heads + 8) * (T / 32, rounded up, + 7) < 2^26 (the threads of a launch). */
 typedef struct { int B, T, heads, dh; int dtype; int buckets; float p; unsigned site; } cnnk_rel_desc;
 int cnnk_rel_attention_fwd(const cnnk_rel_desc* d, const void* qkv, const float* table, const void* plan, const int* lens,
                            const unsigned long long* rng, void* o, float* stats, void* stream);
 
 /* dqkv (all of it: zeros past an image's tokens) and dtable [buckets][heads] (overwritten; NULL: not formed).  o, stats: as the forward call left them, with the same lens, rng and plan. */
-size_t cnnk_rel_attention_workspace_bytes(const cnnk_rel_desc* d);              
+size_t cnnk_rel_attention_workspace_bytes(const cnnk_rel_desc* d);
 int cnnk_rel_attention_bwd(const cnnk_rel_desc* d, const void* qkv, const void* o, const void* d_o,
                            const float* table, const void* plan, const int* lens, const unsigned long long* rng,
                            const float* stats, void* dqkv, float* dtable, void* ws, size_t ws_bytes, void* stream);

@@ -168,3 +168,13 @@ def test_gradients_of_the_oracle_against_differences():
             d = np.zeros_like(table)
             d[k, c] = h
             assert abs((f(qkv, table + d) - f(qkv, table - d)) / (2 * h) - r["dtable"][k, c]) < 1e-7
+
+
+def test_attention_refuses_more_threads_than_a_launch_can_have():
+    D = lambda B, T, heads: rel.rel_desc(B, T, heads, 16, rel.BF16, 0, 0.0, 0)
+    for B, T, heads in ((13421772, 130, 1), (67108863, 1, 1), (33554431, 64, 1), (2 ** 31 - 1, 1, 65535)):
+        assert rel.cnnk_rel_attention_workspace_bytes(D(B, T, heads)) == 0
+    for B, T, heads in ((8388599, 1, 1), (128, 1, 65535), (5592396, 130, 1)):
+        tiles = (T + 31) // 32
+        assert (B * heads + 8) * (tiles + 7) < 2 ** 26
+        assert rel.cnnk_rel_attention_workspace_bytes(D(B, T, heads)) > 0
