@@ -3,36 +3,43 @@
 #include "rel_attention.h"
 
 namespace {
-// Sums of a block's pairs over the workgroups' slots, then of its runs of one bucket.  A wavefront to a block and `heads_of` heads; the block's sums go through LDS in the
+// Sums of a block's pairs over the workgroups' slots, then of its runs of one bucket.  A wavefront to a block and a head; the block's sums go through LDS in the
 // plan's order, sixteen to a lane, and its runs to the block's place in the first slot.  A grid's map leaves 100 to 200 runs of 1024 pairs, so that the
-// gather behind this moves that much less (4096 tokens, 12 heads: 695 us for a gather of all pairs, 239 and 57 this way).
-__global__ void __launch_bounds__(256) rel_runs_kernel(RelArgs a, float* pairs, int units, int heads_of) {
+// gather behind this moves that much less (4096 tokens, 12 heads: 695 us for a gather of all pairs, 204 and 57 this way).  Memory bounds it.
+__global__ void __launch_bounds__(256) rel_runs_kernel(RelArgs a, float* pairs, int units) {
   __shared__ __align__(16) float sm[4][1024];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, blocks = a.NT * a.NT, block = blockIdx.x * 4 + wave;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, blocks = a.NT * a.NT, block = blockIdx.x * 4 + wave, h = blockIdx.y;
   if (block >= blocks) return;
   const uint4* op = reinterpret_cast<const uint4*>(a.order + (size_t)block * 1024 + lane * 16);
   const uint4 o0 = op[0], o1 = op[1];
   const unsigned ends = a.ends[(size_t)block * 64 + lane];
   if (!__any(ends & 0xffffu)) return;       // masked pairs only: no walk has been there
-  const int h1 = min(a.heads, ((int)blockIdx.y + 1) * heads_of);
-  for (int h = blockIdx.y * heads_of; h < h1; ++h) {
-    float* m = pairs + ((size_t)h * blocks + block) * 1024;
-    float4 s[4];
+  float* m = pairs + ((size_t)h * blocks + block) * 1024;
+  const size_t slot = (size_t)a.heads * blocks * 1024;
+  const int slots = rel_groups(h, a.B, units);
+  float4 s[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) s[k] = *reinterpret_cast<const float4*>(m + k * 256 + lane * 4);
-    const int slots = rel_groups(h, a.B, units);
-    for (int x = 1; x < slots; ++x) {
-      const float* n = m + (size_t)x * a.heads * blocks * 1024;
+  for (int k = 0; k < 4; ++k) s[k] = *reinterpret_cast<const float4*>(m + k * 256 + lane * 4);
+  int x = 1;
+  for (; x + 3 < slots; x += 4) {      // in flight together
+    float4 v[4][4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float4 v = *reinterpret_cast<const float4*>(n + k * 256 + lane * 4);
-        s[k].x += v.x, s[k].y += v.y, s[k].z += v.z, s[k].w += v.w;
-      }
-    }
-    const int runs = rel_block_runs(sm[wave], s, o0, o1, ends, lane);
-    for (int k = lane; k < runs; k += 64) m[k] = sm[wave][k];
-    __builtin_amdgcn_wave_barrier();
+    for (int y = 0; y < 4; ++y)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[y][k] = *reinterpret_cast<const float4*>(m + (x + y) * slot + k * 256 + lane * 4);
+#pragma unroll
+    for (int y = 0; y < 4; ++y)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) s[k].x += v[y][k].x, s[k].y += v[y][k].y, s[k].z += v[y][k].z, s[k].w += v[y][k].w;
   }
+  for (; x < slots; ++x)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float4 v = *reinterpret_cast<const float4*>(m + x * slot + k * 256 + lane * 4);
+      s[k].x += v.x, s[k].y += v.y, s[k].z += v.z, s[k].w += v.w;
+    }
+  const int runs = rel_block_runs(sm[wave], s, o0, o1, ends, lane);
+  for (int k = lane; k < runs; k += 64) m[k] = sm[wave][k];
 }
 
 // `lanes` threads to a bucket and head, which take its runs by turns; a workgroup has neighbouring buckets, whose runs lie beside each other
@@ -72,7 +79,8 @@ int check(const cnnk_rel_desc* d, RelDrop* dr) {
   if (d->dtype != CNNK_F32 && d->dtype != CNNK_BF16) return CNNK_ERR_UNSUPPORTED;
   if (d->dh != 16 && d->dh != 32 && d->dh != 64 && d->dh != 128) return CNNK_ERR_UNSUPPORTED;
   if (d->T > 2 * kRelMaxT || (d->buckets && (d->T > kRelMaxT || d->buckets > kRelMaxBuckets))) return CNNK_ERR_UNSUPPORTED;
-  if (d->heads > 65535 || (double)d->T * 3 * d->heads * d->dh * elem_size(d->dtype) >= 2147483648.0 || (double)d->B * d->heads * ((d->T + 31) / 32) > 2147483647.0 / 32) return CNNK_ERR_UNSUPPORTED;
+  if (d->heads > 65535 || (double)d->T * 3 * d->heads * d->dh * elem_size(d->dtype) >= 2147483648.0) return CNNK_ERR_UNSUPPORTED;
+  if (((double)d->B * d->heads + 8) * ((d->T + 31) / 32 + 7) >= 67108864.0) return CNNK_ERR_UNSUPPORTED;
   return CNNK_OK;
 }
 RelArgs args_of(const cnnk_rel_desc* d, RelDrop dr, const float* table, const void* plan, const int* lens, const unsigned long long* rng) {
@@ -118,7 +126,8 @@ RelArgs args_of(const cnnk_rel_desc* d, RelDrop dr, const float* table, const vo
 // scratch of the backward pass: three floats for each row, and the sums of every pair, as often as a head's images lie in different workgroups
 size_t rows_bytes(const cnnk_rel_desc* d) { return align_up((size_t)d->B * d->heads * 3 * ((d->T + 63) / 64 * 64) * 4, 256); }
 // (head, image) pairs to a workgroup of the walk for dk and dv: as many as give every workgroup that the device holds (two to a CU, or one with heads of 128 or a
-// large table) the same number, so that there is one round of them and few sums to add up.
+// large table) the same number, so that there is one round of them and few sums to add up (64 images of 197 tokens, 12 heads of 64: the walk 77 us, 87 with one pair to a
+// workgroup).
 int units_of(const cnnk_rel_desc* d) {
   const long NT = (d->T + 31) / 32, held = d->dh == 128 || d->buckets > 10000 ? 256 : 512;
   const long units = ((long)d->B * d->heads * ((NT + 3) / 4) + held - 1) / held;
@@ -172,9 +181,9 @@ extern "C" int cnnk_rel_attention_bwd(const cnnk_rel_desc* d, const void* qkv, c
                     ? rel_mfma_bwd(a, (const bf16_t*)qkv, (const bf16_t*)o, (const bf16_t*)d_o, stats, (bf16_t*)dqkv, rows, pairs, units, &runs, st)
                     : rel_mfma_bwd(a, (const float*)qkv, (const float*)o, (const float*)d_o, stats, (float*)dqkv, rows, pairs, units, &runs, st);
   if (r != CNNK_OK || !pairs) return r;
-  const int blocks = a.NT * a.NT, heads_of = (int)((long)blocks * d->heads >= 65536 ? 4 : 1);
-  if (!runs) rel_runs_kernel<<<dim3((blocks + 3) / 4, (d->heads + heads_of - 1) / heads_of), 256, 0, st>>>(a, pairs, units, heads_of);
-  // enough threads to fill the device where buckets are few
+  const int blocks = a.NT * a.NT;
+  if (!runs) rel_runs_kernel<<<dim3((blocks + 3) / 4, d->heads), 256, 0, st>>>(a, pairs, units);
+  // enough threads to fill the device where buckets are few (732 buckets, 12 heads: 16 threads 3.9 us, 64 4.9)
   int lanes = 8;
   while (lanes < 256 && (long)d->buckets * d->heads * lanes < 131072) lanes *= 2;
   rel_buckets_kernel<<<dim3((d->buckets + 256 / lanes - 1) / (256 / lanes), d->heads), 256, 0, st>>>(a, pairs, lanes, dtable);
