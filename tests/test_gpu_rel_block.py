@@ -297,3 +297,45 @@ def test_a_row_with_one_key_gives_no_gradient_to_scores(K, dtype, p):
     want = torch.zeros_like(g, dtype=torch.float32)
     want[:, key] = (g.float().view(B, T, heads, dh) * (kept * factor)[..., None]).view(B, T, dim)
     assert ((dq[..., 2 * dim:].float() - want).abs() <= want.abs() * (2.0 ** -8 if dtype == "bf16" else 2.0 ** -21) * 1.01).all()
+
+
+@pytest.mark.parametrize("dtype,dh,T", [("bf16", 64, 3050), ("bf16", 16, 4100), ("f32", 32, 3300)])
+def test_a_long_image_alone_and_in_a_batch(K, dtype, dh, T):
+    """With dropout, captured: the image alone and with an empty one behind it have the same draws, so that o, dq, dk and dv are the same bits and dtable the same sums
+    in another order.  A bucket's T * T / 91 = N terms of either sign add up to about sqrt(N) of one; in chains of N / 64 and more lanes their roundings are at most
+    2^-24 N / 64 * sqrt(64) of one, together 2^-24 sqrt(N) / 8 = 2^-18.3 of the sum for N = 185000, and there are two such sums: 2^-17."""
+    heads, n, t = 12, 16129, torch.bfloat16 if dtype == "bf16" else torch.float32
+    gen = torch.Generator(device=DEV).manual_seed(T)
+    bucket = torch.randint(-1, 90, (T, T), generator=gen, device=DEV, dtype=torch.int32)
+    table, plan = torch.randn(n, heads, generator=gen, device=DEV), K.make_plan(bucket, n)
+    rng = torch.tensor([11, 5], dtype=torch.int64, device=DEV)
+    qkv, g = torch.randn(2, T, 3 * heads * dh, generator=gen, device=DEV).to(t), torch.randn(2, T, heads * dh, generator=gen, device=DEV).to(t)
+
+    def buffers(B):
+        d = K.rel_desc(B, T, heads, dh, K.BF16 if dtype == "bf16" else K.F32, n, 0.15, 9)
+        return d, torch.zeros_like(g[:B]), torch.zeros(B, heads, T, 2, device=DEV), torch.zeros_like(qkv[:B]), torch.zeros_like(table), torch.empty(K.cnnk_rel_attention_workspace_bytes(d), dtype=torch.uint8, device=DEV)
+
+    def step(B, lens, buf):
+        d, o, stats, dq, dt, ws = buf
+        st = torch.cuda.current_stream().cuda_stream
+        K.cnnk_rel_attention_fwd(d, qkv, table, plan, lens, rng, o, stats, st)
+        K.cnnk_rel_attention_bwd(d, qkv, o, g, table, plan, lens, rng, stats, dq, dt, ws, ws.numel(), st)
+
+    batch, alone = buffers(2), buffers(1)
+    step(2, torch.tensor([T, 0], dtype=torch.int32, device=DEV), batch)
+    step(1, None, alone)
+    torch.cuda.synchronize()
+    assert torch.equal(alone[1][0], batch[1][0]) and torch.equal(alone[3][0], batch[3][0]) and torch.equal(alone[2][0], batch[2][0])
+    assert float((alone[4].double() - batch[4].double()).norm() / batch[4].double().norm()) <= 2.0 ** -17
+    kept = alone[4].clone()
+    graph, stream = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=stream):
+        step(1, None, alone)
+    for k in range(3):
+        for x in alone[1:]:
+            x.fill_(k)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(alone[4], kept) and torch.equal(alone[3][0], batch[3][0])
+        (torch.randn(500, 500, device=DEV) @ torch.randn(500, 500, device=DEV)).sum().item()
