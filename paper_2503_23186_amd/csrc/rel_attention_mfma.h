@@ -325,11 +325,21 @@ __device__ __forceinline__ void draws_by_key(unsigned (&word)[8], int query0, un
 }
 
 // What a workgroup works on: which of `groups` (false: none) and which part of it.  The parts of one run on one XCD (every 8th workgroup shares its L2),
-// one behind the other.
+// one behind the other.  The last groups, where they are fewer than the XCDs, are dealt out by parts, so that each XCD has the same share: 36 heads of 1600 tokens 129 -> 91 us
+// forward, 199 -> 135 for dk and dv.  Not where every workgroup has a CU of its own (32 to an XCD) either way: 12 heads of 1024 tokens take 39 us forward, dealt out 42, since
+// two L2s read such a head.
+__host__ __device__ __forceinline__ int whole_groups(int groups, int parts) { return (groups + 7) / 8 * parts > 32 ? groups >> 3 : (groups + 7) >> 3; }      // of an XCD
+__host__ __device__ __forceinline__ int last_share(int groups, int whole, int parts) { return groups > whole * 8 ? ((groups - whole * 8) * parts + 7) >> 3 : 0; }
 __device__ __forceinline__ bool group_part(int groups, FastDiv parts, int* group, int* part) {
+  const int x = blockIdx.x & 7, y = (int)blockIdx.x >> 3, n = parts.d, whole = whole_groups(groups, n);
   int g;
-  parts.divmod((int)blockIdx.x >> 3, &g, part);
-  *group = g * 8 + (blockIdx.x & 7);
+  if (y < whole * n) {
+    parts.divmod(y, &g, part);
+    *group = g * 8 + x;
+  } else {
+    parts.divmod(x * last_share(groups, whole, n) + y - whole * n, &g, part);
+    *group = whole * 8 + g;
+  }
   return *group < groups;
 }
 __device__ __forceinline__ float both_halves_max(float v) {
@@ -748,6 +758,10 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
   }
 }
 
+int grid_of(int groups, int parts) {
+  const int whole = whole_groups(groups, parts);
+  return (whole * parts + last_share(groups, whole, parts)) * 8;
+}
 template <typename Kern> int allow_lds(Kern kern, size_t bytes) {      // more than 64 KB has to be asked for, on the device that is current
   if (bytes <= 65536) return CNNK_OK;
   return hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess ? CNNK_OK : CNNK_ERR_HIP;
@@ -766,7 +780,7 @@ int fwd_launch(const RelArgs& a, const T* qkv, T* o, float* stats, hipStream_t s
   const int waves = waves_of(a, lds, true), parts = (a.NT + waves - 1) / waves, pairs = a.B * a.heads;
   const auto kern = rel_mfma_fwd_kernel<T, DH, BIAS, DROP>;
   if (allow_lds(kern, lds) != CNNK_OK) return CNNK_ERR_HIP;
-  kern<<<(pairs + 7) / 8 * 8 * parts, 64 * waves, lds, st>>>(a, qkv, o, stats, fast_div(parts));
+  kern<<<grid_of(pairs, parts), 64 * waves, lds, st>>>(a, qkv, o, stats, fast_div(parts));
   return launch_status();
 }
 template <typename T, int DH, bool BIAS, bool DROP>
@@ -784,8 +798,8 @@ int bwd_launch(const RelArgs& a, const T* qkv, const T* o, const T* d_o, const f
   if constexpr (BIAS && DH <= 64)
     if (*runs) dkv = rel_mfma_dkv_kernel<T, DH, BIAS, DROP, true>;
   if (allow_lds(dq, lds) != CNNK_OK || allow_lds(dkv, lds_kv + lds_runs) != CNNK_OK) return CNNK_ERR_HIP;
-  dq<<<(heads + 7) / 8 * 8 * parts, 64 * waves, lds, st>>>(a, qkv, o, d_o, stats, dqkv, rows, fast_div(parts));
-  dkv<<<((heads + units - 1) / units + 7) / 8 * 8 * parts, 64 * waves, lds_kv + lds_runs, st>>>(a, qkv, d_o, rows, dqkv, pairs, fast_div(parts), units, (heads + units - 1) / units,
+  dq<<<grid_of(heads, parts), 64 * waves, lds, st>>>(a, qkv, o, d_o, stats, dqkv, rows, fast_div(parts));
+  dkv<<<grid_of((heads + units - 1) / units, parts), 64 * waves, lds_kv + lds_runs, st>>>(a, qkv, d_o, rows, dqkv, pairs, fast_div(parts), units, (heads + units - 1) / units,
                                                                                                                (unsigned)lds_kv);
   return launch_status();
 }
