@@ -472,11 +472,11 @@ __global__ void __launch_bounds__(512, sizeof(T) == 2 && DH <= 64 ? 4 : 2) rel_m
   }
   if (q0 >= a.T) return;
   l = both_halves_sum(l);
-  const bool any = q < n && l > 0.f;
+  const bool any = q < n && !(l == 0.f);      // 0: every key masked, since the largest score adds 2^-down at least; NaN (in q, k or the table, or an overflow) is handed on
   scale_rows<D::NM>(oacc, a.dr.scale / l, any);
   D::store(o + ((size_t)b * a.T + q) * d + head * DH, oacc, h, q < a.T);
   if (stats && h == 0 && q < a.T)
-    *reinterpret_cast<float2*>(stats + ((size_t)bh * a.T + q) * 2) = any ? float2{m, kLn2 * __builtin_amdgcn_logf(l * a.up)} : float2{-INFINITY, 0.f};
+    *reinterpret_cast<float2*>(stats + ((size_t)bh * a.T + q) * 2) = any ? float2{m > -INFINITY ? m : 0.f, kLn2 * __builtin_amdgcn_logf(l * a.up)} : float2{-INFINITY, 0.f};
 }
 
 // ---- backward: dq, and for the kernel behind it the rows' statistics and delta -----------------------------------------------
