@@ -170,7 +170,7 @@ extern "C" int cnnk_rel_attention_bwd(const cnnk_rel_desc* d, const void* qkv, c
   if (!qkv || !o || !d_o || !stats || !dqkv || (d->buckets && (!table || !plan)) || (dr.q && !rng)) return CNNK_ERR_NULL;
   if (!ws || ws_bytes < cnnk_rel_attention_workspace_bytes(d)) return CNNK_ERR_WORKSPACE;
   if (!rel_aligned(qkv, 16) || !rel_aligned(o, 16) || !rel_aligned(d_o, 16) || !rel_aligned(stats, 8) || !rel_aligned(table, 4) ||
-      !rel_aligned(plan, 256) || !rel_aligned(lens, 4) || !rel_aligned(rng, 8) || !rel_aligned(dqkv, 16) || !rel_aligned(dtable, 4) || !rel_aligned(ws, 256))
+      !rel_aligned(plan, 256) || !rel_aligned(lens, 4) || !rel_aligned(rng, 8) || !rel_aligned(dqkv, 16) || !rel_aligned(dtable, 4) || !rel_aligned(ws, 16))
     return CNNK_ERR_UNSUPPORTED;
   const RelArgs a = args_of(d, dr, table, plan, lens, rng);
   float *rows = (float*)ws, *pairs = d->buckets && dtable ? (float*)((char*)ws + rows_bytes(d)) : nullptr;

@@ -71,3 +71,58 @@ def test_a_table_that_is_not_a_number(K, dtype, T):
     assert (torch.isnan(o.view(2, T, heads, 64)).all(-1) == bad).all() and (torch.isnan(m[..., 1]) == bad.permute(0, 2, 1)).all()
     assert torch.equal(o.view(2, T, heads, 64)[~bad], good.view(2, T, heads, 64)[~bad])
     assert torch.isnan(dq.view(2, T, 3, heads, 64)[:, :, 0][bad]).all() and torch.isnan(dt[4, 1]) and torch.isfinite(dt[:, 0]).all()
+
+
+# ---- addresses -------------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,T", [("bf16", 45), ("f32", 130)])
+def test_every_alignment_that_is_asked_for_is_enough(K, dtype, T):
+    """Activations and workspaces 16 bytes off a line, statistics 8, the table, its gradient and the lengths 4: the bits of aligned ones."""
+    bucket, n = map_of("grid", T)
+    c = Case(K, dtype, 2, T, 2, 32, bucket, n, 0.1, lens=[T, T - 9])
+    o, m = c.fwd()
+    dq, dt = c.bwd(o, m)
+
+    def off(t, by):
+        raw = torch.empty(t.numel() * t.element_size() + 256, dtype=torch.uint8, device=DEV)
+        return raw[by:by + t.numel() * t.element_size()].view(t.dtype).view(t.shape) if by % t.element_size() == 0 else None
+
+    def moved(t, by):
+        x = off(t, by)
+        x.copy_(t)
+        return x
+
+    c.gq, c.gg, c.gt, c.gl, c.s = moved(c.gq, 16), moved(c.gg, 48), moved(c.gt, 4), moved(c.gl, 4), moved(c.s, 8)
+    o2, m2, dq2, dt2 = off(o, 16), off(m, 8), off(dq, 80), off(dt, 12)
+    need = K.cnnk_rel_attention_workspace_bytes(c.desc)
+    ws = torch.full((need + 512,), 255, dtype=torch.uint8, device=DEV)
+    for at in (16, 240):
+        K.cnnk_rel_attention_fwd(c.desc, c.gq, c.gt, c.plan, c.gl, c.s, o2, m2)
+        K.cnnk_rel_attention_bwd(c.desc, c.gq, o2, c.gg, c.gt, c.plan, c.gl, c.s, m2, dq2, dt2, ws[at:], need)
+        for a, b in ((o, o2), (m, m2), (dq, dq2), (dt, dt2)):
+            assert torch.equal(a, b)
+    wp = torch.empty(K.cnnk_rel_plan_workspace_bytes(T, n) + 16, dtype=torch.uint8, device=DEV)
+    plan, bm = torch.empty_like(c.plan), moved(torch.from_numpy(np.ascontiguousarray(bucket, dtype=np.int32)).to(DEV), 4)
+    K.cnnk_rel_plan(T, n, bm, plan, wp[16:], wp.numel() - 16)
+    c.plan = plan
+    assert torch.equal(c.fwd()[0], o)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_dropout_at_every_alignment_that_is_asked_for(K, dtype):
+    rows, C, t = 70, 264, torch.bfloat16 if dtype == "bf16" else torch.float32
+    g = torch.Generator(device=DEV).manual_seed(1)
+    rand = lambda *s: torch.randn(*s, generator=g, device=DEV)
+    z, res, bias, s = rand(rows, C).to(t), rand(rows, C).to(t), rand(C), torch.tensor([3, 4], device=DEV)
+    d = K.dropout_desc(rows, C, K.BF16 if dtype == "bf16" else K.F32, 0.3, 2)
+    need = K.cnnk_dropout_workspace_bytes(d)
+    got = []
+    for by, small in ((0, 0), (16, 4), (112, 12)):
+        at = lambda x, k: torch.empty(x.numel() * x.element_size() + 256, dtype=torch.uint8, device=DEV)[k:k + x.numel() * x.element_size()].view(x.dtype).view(x.shape).copy_(x)
+        a, r, b, st = at(z, by), at(res, by), at(bias, by), at(s, by % 16 + 8 if by else 0)
+        y, dz, db = at(z, by), at(z, by), at(bias, small)
+        K.cnnk_dropout_fwd(d, a, b, r, st, y)
+        K.cnnk_dropout_bwd(d, a, st, dz, db, at(torch.zeros(need, dtype=torch.uint8, device=DEV), by), need)
+        got.append((y, dz, db))
+    for other in got[1:]:
+        assert all(torch.equal(x, y) for x, y in zip(other, got[0]))
