@@ -51,7 +51,8 @@ int cnnk_dropout_bwd(const cnnk_dropout_desc* d, const void* dy, const unsigned 
  * (2 gw - 1) + xt - xu + gw - 1; with cls != 0 a class token in front of them has buckets n = (2 gh - 1)(2 gw - 1) (its keys
  * among the patches), n + 1 (it as a key) and n + 2 (itself).
  * cnnk_rel_plan lays a map out for the calls below (which pairs a bucket has, and the map in the order in which they read it).
- * A program makes a plan once for each map; `plan` is device memory of cnnk_rel_plan_bytes, 256-byte aligned.
+ * A program makes a plan once for each map; `plan` is device memory of cnnk_rel_plan_bytes, 256-byte aligned.  It holds its T and buckets: a
+ * call whose descriptor has others (its plan being memory of that many bytes all the same) gives NaN for every token and in all of dtable.
  * 1 <= T <= 8192, 1 <= buckets <= 16382. */
 int cnnk_rel_buckets_grid(int gh, int gw, int cls, int* bucket, void* stream);
 size_t cnnk_rel_plan_bytes(int T, int buckets);                  /* 0: unsupported */

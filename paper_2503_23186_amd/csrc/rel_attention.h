@@ -17,7 +17,7 @@ struct RelArgs {
   const float* table;
   const unsigned short *by_query, *by_key, *order;
   const unsigned* ends;
-  const int* dead;
+  const int* about;
   const unsigned long long *live_query, *live_key;
   const int *start, *list, *lens;
   const unsigned long long* rng;
@@ -27,6 +27,14 @@ __device__ __forceinline__ int rel_tokens(const RelArgs& a, int b) {
   if (!a.lens) return a.T;
   const int n = a.lens[b];
   return n < 0 ? 0 : n > a.T ? a.T : n;
+}
+
+// Whether the plan is one for the call's T and buckets, which a call cannot see before it is enqueued: with another its results are NaN, and nothing that the plan holds
+// becomes an address.  *dead: blocks that are masked as a whole.
+__device__ __forceinline__ bool rel_plan_fits(const RelArgs& a, int* dead) {
+  const int4 p = *reinterpret_cast<const int4*>(a.about);
+  *dead = __builtin_amdgcn_readfirstlane(p.x);
+  return __builtin_amdgcn_readfirstlane((p.y ^ kRelPlanMark) | (p.z ^ a.T) | (p.w ^ a.buckets)) == 0;      // all lanes': scalar
 }
 
 // A block's sums by runs of one bucket (the plan's order): four quads of a lane in, the runs' sums out, one behind the other in the wavefront's 4 KB of LDS;

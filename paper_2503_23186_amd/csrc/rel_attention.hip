@@ -13,7 +13,8 @@ __global__ void __launch_bounds__(256) rel_runs_kernel(RelArgs a, float* pairs, 
   const uint4* op = reinterpret_cast<const uint4*>(a.order + (size_t)block * 1024 + lane * 16);
   const uint4 o0 = op[0], o1 = op[1];
   const unsigned ends = a.ends[(size_t)block * 64 + lane];
-  if (!__any(ends & 0xffffu)) return;       // masked pairs only: no walk has been there
+  int dead;
+  if (!rel_plan_fits(a, &dead) || !__any(ends & 0xffffu)) return;       // masked pairs only: no walk has been there
   float* m = pairs + ((size_t)h * blocks + block) * 1024;
   const size_t slot = (size_t)a.heads * blocks * 1024;
   const int slots = rel_groups(h, a.B, units);
@@ -48,8 +49,10 @@ __global__ void __launch_bounds__(256) rel_buckets_kernel(RelArgs a, const float
   __shared__ float sm[256];
   const int per = 256 / lanes, k = blockIdx.x * per + threadIdx.x / lanes, h = blockIdx.y, j = threadIdx.x & (lanes - 1);
   const float* m = pairs + (size_t)h * a.NT * a.NT * 1024;
-  float s = 0.f;
-  if (k < a.buckets) {
+  int dead;
+  const bool fits = rel_plan_fits(a, &dead);
+  float s = fits ? 0.f : NAN;
+  if (fits && k < a.buckets) {
     const int s1 = a.start[k + 1];
     int i = a.start[k] + j;
     for (; i + 3 * lanes < s1; i += 4 * lanes) {
@@ -105,7 +108,7 @@ RelArgs args_of(const cnnk_rel_desc* d, RelDrop dr, const float* table, const vo
   a.by_query = a.by_key = a.order = nullptr;
   a.ends = nullptr;
   a.live_query = a.live_key = nullptr;
-  a.dead = nullptr;
+  a.about = nullptr;
   a.start = a.list = nullptr;
   a.lens = lens;
   a.rng = rng;
@@ -115,7 +118,7 @@ RelArgs args_of(const cnnk_rel_desc* d, RelDrop dr, const float* table, const vo
     a.by_key = (const unsigned short*)((const char*)plan + at.by_key);
     a.order = (const unsigned short*)((const char*)plan + at.order);
     a.ends = (const unsigned*)((const char*)plan + at.ends);
-    a.dead = (const int*)((const char*)plan + at.dead);
+    a.about = (const int*)((const char*)plan + at.about);
     a.live_query = (const unsigned long long*)((const char*)plan + at.live_query);
     a.live_key = (const unsigned long long*)((const char*)plan + at.live_key);
     a.start = (const int*)((const char*)plan + at.start);

@@ -237,7 +237,7 @@ struct Live {
 template <bool BIAS>
 __device__ __forceinline__ Live live_start(unsigned char* lds, const unsigned long long* p, int dead, int block0, int NT, int wave, int lane) {
   unsigned long long* m = reinterpret_cast<unsigned long long*>(lds);
-  Live l = {m + wave * 4, m + 32, BIAS && __builtin_amdgcn_readfirstlane(dead) != 0};
+  Live l = {m + wave * 4, m + 32, BIAS && dead != 0};
   if (l.some) {
     if (threadIdx.x < 32) {
       const unsigned long long v = block0 + (lane >> 2) < NT ? p[(size_t)block0 * 4 + lane] : 0;      // word lane % 4 of block lane / 4
@@ -388,6 +388,7 @@ __global__ void __launch_bounds__(512, sizeof(T) == 2 && DH <= 64 ? 4 : 2) rel_m
 #pragma unroll
   for (int mt = 0; mt < D::NM; ++mt) oacc[mt] = zero16();
   float m = -INFINITY, l = 0.f;      // l: of this lane's half of the keys
+  bool fits = true;
   if (first < n) {
     float* table = reinterpret_cast<float*>(smem + 2 * D::STAGE);
     Stager<T, DH> st;
@@ -399,7 +400,7 @@ __global__ void __launch_bounds__(512, sizeof(T) == 2 && DH <= 64 ? 4 : 2) rel_m
     MapRegs mr, next;
     int dead = 0;
     if (BIAS) {
-      dead = *a.dead;
+      fits = rel_plan_fits(a, &dead);
       if (mine) map_load(next, map, 0, lane);
       table_load(2 * D::STAGE, table, a, head, wave, waves, lane);
     }
@@ -415,7 +416,7 @@ __global__ void __launch_bounds__(512, sizeof(T) == 2 && DH <= 64 ? 4 : 2) rel_m
       const int t = live_next(live.all, live.some, k * TS, tiles);
       return t < tiles ? t / TS : stages;
     };
-    int tn = mine ? tile_from(0) : tiles;
+    int tn = mine && fits ? tile_from(0) : tiles;
     if (BIAS && tn > 0 && tn < tiles) map_load(next, map, tn, lane);
     for (int stage = 0, buf = 0; stage < stages; buf ^= 1) {
       wait_vm<0>();
@@ -471,7 +472,7 @@ __global__ void __launch_bounds__(512, sizeof(T) == 2 && DH <= 64 ? 4 : 2) rel_m
     }
   }
   if (q0 >= a.T) return;
-  l = both_halves_sum(l);
+  l = fits ? both_halves_sum(l) : NAN;
   const bool any = q < n && !(l == 0.f);      // 0: every key masked, since the largest score adds 2^-down at least; NaN (in q, k or the table, or an overflow) is handed on
   scale_rows<D::NM>(oacc, a.dr.scale / l, any);
   D::store(o + ((size_t)b * a.T + q) * d + head * DH, oacc, h, q < a.T);
@@ -502,6 +503,7 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, sizeof(T) == 2 && DH <= 
 #pragma unroll
   for (int mt = 0; mt < D::NM; ++mt) dq[mt] = zero16();
   float m = 0.f, L2 = INFINITY, delta = 0.f, lack = 0.f;
+  bool fits = true;
   if (first < n) {
     float* table = reinterpret_cast<float*>(smem + 2 * D::STAGE);
     Stager<T, DH> st;
@@ -513,7 +515,7 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, sizeof(T) == 2 && DH <= 
     MapRegs mr, next;
     int dead = 0;
     if (BIAS) {
-      dead = *a.dead;
+      fits = rel_plan_fits(a, &dead);
       if (mine) map_load(next, map, 0, lane);
       table_load(2 * D::STAGE, table, a, head, wave, waves, lane);
     }
@@ -542,7 +544,7 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, sizeof(T) == 2 && DH <= 
       const int t = live_next(live.all, live.some, k * TS, tiles);
       return t < tiles ? t / TS : stages;
     };
-    int tn = mine ? tile_from(0) : tiles;
+    int tn = mine && fits ? tile_from(0) : tiles;
     if (BIAS && tn > 0 && tn < tiles) map_load(next, map, tn, lane);
     for (int stage = 0, buf = 0; stage < stages; buf ^= 1) {
       wait_vm<0>();
@@ -586,7 +588,7 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, sizeof(T) == 2 && DH <= 
   }
   if (q0 >= a.T) return;
   lack = both_halves_sum(lack);
-  scale_rows<D::NM>(dq, a.scale * a.dr.scale, q < n);
+  scale_rows<D::NM>(dq, fits ? a.scale * a.dr.scale : NAN, q < n);
   D::store(dqkv + (size_t)b * a.T * ld + head * DH + (size_t)q * ld, dq, h, q < a.T);
   if (h == 0) {
     float* r = rows + (size_t)bh * 3 * a.Tp + q;
@@ -620,9 +622,23 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
   RelKey key{0u, 0u};
   if (DROP) key = rel_key(a.rng, a.site);
   const unsigned short* map = BIAS ? a.by_key + (size_t)(u0 >> 5) * a.NT * 1024 : nullptr;
-  const Live live = live_start<BIAS>(reinterpret_cast<unsigned char*>(table + a.buckets + 1 + (a.buckets + 1 & 1)), a.live_key, BIAS ? *a.dead : 0, first >> 5, a.NT,
-                                     wave, lane);
+  int dead = 0;
   const int end = min(all, (group + 1) * units);
+  if (BIAS && !rel_plan_fits(a, &dead)) {
+    f32x16_t none[D::NM];
+#pragma unroll
+    for (int mt = 0; mt < D::NM; ++mt) none[mt] = zero16();
+    for (int unit = group * units; unit < end; ++unit) {
+      const int head = a.by_images.div(unit), b = unit - head * a.B;
+      T* out = dqkv + (size_t)b * a.T * ld + head * DH + d + (size_t)u * ld;
+      if (u0 >= a.T) return;
+      scale_rows<D::NM>(none, NAN, u < rel_tokens(a, b));
+      D::store(out, none, h, u < a.T);
+      D::store(out + d, none, h, u < a.T);
+    }
+    return;
+  }
+  const Live live = live_start<BIAS>(reinterpret_cast<unsigned char*>(table + a.buckets + 1 + (a.buckets + 1 & 1)), a.live_key, dead, first >> 5, a.NT, wave, lane);
   int head = a.by_images.div(group * units), b = group * units - head * a.B;
   bool fresh = true;                 // the first image of its head here
   for (int unit = group * units; unit < end; ++unit, ++b) {

@@ -103,7 +103,13 @@ def rel_desc(B, T, heads, dh, dtype, buckets=0, p=0.0, site=0):
     return RelDesc(B, T, heads, dh, dtype, buckets, p, site)
 
 
+def _check_plan(d, plan):
+    if d.buckets > 0 and isinstance(plan, torch.Tensor) and plan.numel() * plan.element_size() < lib.cnnk_rel_plan_bytes(d.T, d.buckets):
+        raise ValueError("the plan is too small for %d tokens and %d buckets" % (d.T, d.buckets))
+
+
 def cnnk_rel_attention_fwd(d, qkv, table, plan, lens, rng, o, stats=None, stream=0):
+    _check_plan(d, plan)
     _check(lib.cnnk_rel_attention_fwd(C.byref(d), ptr(qkv), ptr(table), ptr(plan), ptr(lens), ptr(rng), ptr(o), ptr(stats), stream), "cnnk_rel_attention_fwd")
 
 
@@ -112,6 +118,7 @@ def cnnk_rel_attention_workspace_bytes(d):
 
 
 def cnnk_rel_attention_bwd(d, qkv, o, d_o, table, plan, lens, rng, stats, dqkv, dtable, ws, ws_bytes, stream=0):
+    _check_plan(d, plan)
     _check(lib.cnnk_rel_attention_bwd(C.byref(d), ptr(qkv), ptr(o), ptr(d_o), ptr(table), ptr(plan), ptr(lens),
                                       ptr(rng), ptr(stats), ptr(dqkv), ptr(dtable), ptr(ws), ws_bytes, stream),
            "cnnk_rel_attention_bwd")

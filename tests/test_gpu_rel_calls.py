@@ -73,6 +73,54 @@ def test_a_table_that_is_not_a_number(K, dtype, T):
     assert torch.isnan(dq.view(2, T, 3, heads, 64)[:, :, 0][bad]).all() and torch.isnan(dt[4, 1]) and torch.isfinite(dt[:, 0]).all()
 
 
+# ---- plans of other maps ---------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,dh,p", [("bf16", 64, 0.0), ("bf16", 32, 0.2), ("f32", 16, 0.1), ("bf16", 128, 0.0)])
+@pytest.mark.parametrize("T,other_T,other_n", [(20, 23, 9), (70, 70, 14), (70, 97, 9), (300, 300, 8), (300, 330, 5000)])
+@pytest.mark.parametrize("kind", ["other", "zeros", "ones"])
+def test_a_plan_of_another_map_gives_nan(K, dtype, dh, p, T, other_T, other_n, kind):
+    """Plans of other sizes that have the call's bytes, and memory that holds none: NaN for every token, zeros past an image's end, nothing written elsewhere."""
+    n, heads, lens = 9, 2, [T, T // 2, 0]
+    rng = np.random.default_rng(T)
+    c = Case(K, dtype, 3, T, heads, dh, rng.integers(-1, n, (T, T)).astype(np.int32), n, p, lens=lens)
+    good, size = c.plan, K.cnnk_rel_plan_bytes(T, n)
+    plan = torch.full((max(size, K.cnnk_rel_plan_bytes(other_T, other_n)),), 255 if kind == "ones" else 0, dtype=torch.uint8, device=DEV)
+    if kind == "other":
+        made = K.make_plan(torch.from_numpy(rng.integers(0, other_n, (other_T, other_T)).astype(np.int32)).to(DEV), other_n)
+        plan[:made.numel()] = made
+    o, m = c.fwd()
+    inside = torch.arange(T, device=DEV)[None] < torch.tensor(lens, device=DEV)[:, None]
+    need = K.cnnk_rel_attention_workspace_bytes(c.desc)
+    dq, dt = torch.full_like(c.gq, 9.0), torch.full((n + 2, heads), 9.0, device=DEV)
+    ws = torch.full((need + 1024,), 77, dtype=torch.uint8, device=DEV)
+    K.cnnk_rel_attention_bwd(c.desc, c.gq, o, c.gg, c.gt, plan, c.gl, c.s, m, dq, dt[1:], ws[512:], need)
+    assert torch.isnan(dq[inside]).all() and (dq[~inside] == 0).all() and torch.isnan(dt[1:-1]).all()
+    assert (dt[0] == 9).all() and (dt[-1] == 9).all() and (ws[:512] == 77).all() and (ws[512 + need:] == 77).all()
+    c.plan = plan
+    o2, m2 = c.fwd()
+    assert torch.isnan(o2[inside]).all() and (o2[~inside] == 0).all()
+    assert torch.isnan(m2[..., 1].permute(0, 2, 1)[inside]).all() and torch.isneginf(m2[..., 0].permute(0, 2, 1)[~inside]).all()
+    c.plan = good
+    assert torch.equal(c.fwd()[0], o)
+
+
+@pytest.mark.parametrize("T,n", [(3300, 16129), (4100, 12000)])
+def test_a_long_image_with_a_plan_of_another_map(K, T, n):
+    """One image whose dx becomes runs of a bucket in the walk: a plan of fewer buckets in its place."""
+    heads, dh = 12, 16
+    m = torch.zeros(T, T, dtype=torch.int32, device=DEV)
+    made = K.make_plan(m, n - 70)
+    plan = torch.zeros(K.cnnk_rel_plan_bytes(T, n), dtype=torch.uint8, device=DEV)
+    plan[:made.numel()] = made
+    d = K.rel_desc(1, T, heads, dh, K.BF16, n, 0.0, 0)
+    x = lambda *s: torch.ones(*s, dtype=torch.bfloat16, device=DEV)
+    qkv, o, g, table, stats = x(1, T, 3 * heads * dh), x(1, T, heads * dh), x(1, T, heads * dh), torch.ones(n, heads, device=DEV), torch.zeros(1, heads, T, 2, device=DEV)
+    dq, dt, need = torch.zeros_like(qkv), torch.zeros_like(table), K.cnnk_rel_attention_workspace_bytes(d)
+    ws = torch.full((need + 1024,), 77, dtype=torch.uint8, device=DEV)
+    K.cnnk_rel_attention_bwd(d, qkv, o, g, table, plan, None, None, stats, dq, dt, ws[512:], need)
+    assert torch.isnan(dq).all() and torch.isnan(dt).all() and (ws[:512] == 77).all() and (ws[512 + need:] == 77).all()
+
+
 # ---- addresses -------------------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype,T", [("bf16", 45), ("f32", 130)])
