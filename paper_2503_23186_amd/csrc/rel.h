@@ -55,7 +55,7 @@ static inline bool rel_aligned(const void* p, size_t a) { return ((size_t)p & (a
 // An entry is 4 x bucket, the byte offset into a head's table in LDS; 4 x buckets for masked pairs and for padding, where that table holds -infinity.
 //   live_query, live_key   u64 [NT][4]: bit k of a block of queries (keys): its pairs with block k of the others are not all masked.  The walks
 //             leave the others out.
-//   about     int [4]: how many blocks that are; kRelPlanMark, T and buckets, so that a kernel can tell a plan of other sizes (or memory that holds none)
+//   about     int [2]: how many blocks that are; rel_plan_mark, so that a kernel can tell a plan of other sizes, and memory that holds none
 // What reduces dx of the pairs, summed over images, to buckets.  These sums lie in blocks as in by_key, in a block registers in fours [4][64 lanes][4].
 //   order     u16 [NT][NT][64][16]: a block's pairs sorted by bucket (masked ones last), sixteen to a lane: their bytes in the block
 //   ends      u32 [NT][NT][64]: low half: which of a lane's sixteen end a run of one bucket; high half: runs of the lanes before
@@ -63,7 +63,8 @@ static inline bool rel_aligned(const void* p, size_t a) { return ((size_t)p & (a
 //   start     int [buckets + 1]: where a bucket's runs begin in
 //   list      int [T * T at most]: places of its runs, in the order of the blocks
 constexpr int kRelMaxT = 8192, kRelMaxBuckets = 16382;
-constexpr int kRelPlanMark = 0x6e616c70;      // no entry of a map, order or list: those are multiples of 4 below 2^16, or below 2^26
+// negative and odd: no two entries of a map or an order (multiples of 4), no word of ends, start or list (not negative)
+__host__ __device__ static inline int rel_plan_mark(int T, int buckets) { return ~(T << 16 | buckets << 2); }
 struct RelPlan { size_t by_query, by_key, order, ends, live_query, live_key, about, start, list, bytes; };
 static inline RelPlan rel_plan_layout(int T, int buckets) {
   const size_t NT = (T + 31) / 32, map = NT * NT * 2048;

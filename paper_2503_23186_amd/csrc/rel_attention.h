@@ -7,6 +7,7 @@ static inline FastDiv fast_div(unsigned d) {
   f.init(d);
   return f;
 }
+struct RelAbout { int dead, mark; };         // blocks that are masked as a whole, rel_plan_mark
 struct RelArgs {
   int B, T, Tp, heads, dh, NT, buckets;      // Tp: T rounded up to 64, NT: blocks of 32
   FastDiv by_heads, by_images;
@@ -17,7 +18,7 @@ struct RelArgs {
   const float* table;
   const unsigned short *by_query, *by_key, *order;
   const unsigned* ends;
-  const int* about;
+  const RelAbout* about;
   const unsigned long long *live_query, *live_key;
   const int *start, *list, *lens;
   const unsigned long long* rng;
@@ -30,12 +31,13 @@ __device__ __forceinline__ int rel_tokens(const RelArgs& a, int b) {
 }
 
 // Whether the plan is one for the call's T and buckets, which a call cannot see before it is enqueued: with another its results are NaN, and nothing that the plan holds
-// becomes an address.  *dead: blocks that are masked as a whole.
-__device__ __forceinline__ bool rel_plan_fits(const RelArgs& a, int* dead) {
-  const int4 p = *reinterpret_cast<const int4*>(a.about);
-  *dead = __builtin_amdgcn_readfirstlane(p.x);
-  return __builtin_amdgcn_readfirstlane((p.y ^ kRelPlanMark) | (p.z ^ a.T) | (p.w ^ a.buckets)) == 0;      // all lanes': scalar
+// becomes an address of memory.  The walks load it with the rest and look at it when that is on its way, all five kernels with scalar loads (8 images of 197 tokens, 12 heads:
+// forward 9.6 -> 9.7 us in evaluation, a training step's five kernels 53.4 -> 54.0; compared where it is loaded, 9.9 and 54.0).
+__device__ __forceinline__ RelAbout rel_about(const RelArgs& a) {
+  const auto p = (const __attribute__((address_space(4))) int*)(unsigned long long)a.about;      // constant while a kernel runs
+  return RelAbout{p[0], p[1]};
 }
+__device__ __forceinline__ bool rel_plan_fits(const RelArgs& a, RelAbout about) { return about.mark == rel_plan_mark(a.T, a.buckets); }
 
 // A block's sums by runs of one bucket (the plan's order): four quads of a lane in, the runs' sums out, one behind the other in the wavefront's 4 KB of LDS;
 // returns their number.

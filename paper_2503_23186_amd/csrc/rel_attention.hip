@@ -13,8 +13,7 @@ __global__ void __launch_bounds__(256) rel_runs_kernel(RelArgs a, float* pairs, 
   const uint4* op = reinterpret_cast<const uint4*>(a.order + (size_t)block * 1024 + lane * 16);
   const uint4 o0 = op[0], o1 = op[1];
   const unsigned ends = a.ends[(size_t)block * 64 + lane];
-  int dead;
-  if (!rel_plan_fits(a, &dead) || !__any(ends & 0xffffu)) return;       // masked pairs only: no walk has been there
+  if (!rel_plan_fits(a, rel_about(a)) || !__any(ends & 0xffffu)) return;       // masked pairs only: no walk has been there
   float* m = pairs + ((size_t)h * blocks + block) * 1024;
   const size_t slot = (size_t)a.heads * blocks * 1024;
   const int slots = rel_groups(h, a.B, units);
@@ -49,8 +48,7 @@ __global__ void __launch_bounds__(256) rel_buckets_kernel(RelArgs a, const float
   __shared__ float sm[256];
   const int per = 256 / lanes, k = blockIdx.x * per + threadIdx.x / lanes, h = blockIdx.y, j = threadIdx.x & (lanes - 1);
   const float* m = pairs + (size_t)h * a.NT * a.NT * 1024;
-  int dead;
-  const bool fits = rel_plan_fits(a, &dead);
+  const bool fits = rel_plan_fits(a, rel_about(a));
   float s = fits ? 0.f : NAN;
   if (fits && k < a.buckets) {
     const int s1 = a.start[k + 1];
@@ -118,7 +116,7 @@ RelArgs args_of(const cnnk_rel_desc* d, RelDrop dr, const float* table, const vo
     a.by_key = (const unsigned short*)((const char*)plan + at.by_key);
     a.order = (const unsigned short*)((const char*)plan + at.order);
     a.ends = (const unsigned*)((const char*)plan + at.ends);
-    a.about = (const int*)((const char*)plan + at.about);
+    a.about = (const RelAbout*)((const char*)plan + at.about);
     a.live_query = (const unsigned long long*)((const char*)plan + at.live_query);
     a.live_key = (const unsigned long long*)((const char*)plan + at.live_key);
     a.start = (const int*)((const char*)plan + at.start);

@@ -398,9 +398,9 @@ __global__ void __launch_bounds__(512, sizeof(T) == 2 && DH <= 64 ? 4 : 2) rel_m
     const int tiles = (n + 31) >> 5, stages = (tiles + TS - 1) / TS;
     const unsigned short* map = BIAS ? a.by_query + (size_t)(q0 >> 5) * a.NT * 1024 : nullptr;
     MapRegs mr, next;
-    int dead = 0;
+    RelAbout about = {0, 0};
     if (BIAS) {
-      fits = rel_plan_fits(a, &dead);
+      about = rel_about(a);
       if (mine) map_load(next, map, 0, lane);
       table_load(2 * D::STAGE, table, a, head, wave, waves, lane);
     }
@@ -410,12 +410,13 @@ __global__ void __launch_bounds__(512, sizeof(T) == 2 && DH <= 64 ? 4 : 2) rel_m
     RelKey key{0u, 0u};
     if (DROP) key = rel_key(a.rng, a.site);
     // stages that one of the workgroup's blocks needs, and of them the tiles that this wavefront's does
-    const Live live = live_start<BIAS>(reinterpret_cast<unsigned char*>(table + a.buckets + 1 + (a.buckets + 1 & 1)), a.live_query, dead, first >> 5, a.NT, wave, lane);
+    const Live live = live_start<BIAS>(reinterpret_cast<unsigned char*>(table + a.buckets + 1 + (a.buckets + 1 & 1)), a.live_query, about.dead, first >> 5, a.NT, wave, lane);
     auto tile_from = [&](int t) __attribute__((always_inline)) { return live_next(live.w, live.some, t, tiles); };
     auto stage_from = [&](int k) __attribute__((always_inline)) {
       const int t = live_next(live.all, live.some, k * TS, tiles);
       return t < tiles ? t / TS : stages;
     };
+    if (BIAS) fits = rel_plan_fits(a, about);
     int tn = mine && fits ? tile_from(0) : tiles;
     if (BIAS && tn > 0 && tn < tiles) map_load(next, map, tn, lane);
     for (int stage = 0, buf = 0; stage < stages; buf ^= 1) {
@@ -513,9 +514,9 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, sizeof(T) == 2 && DH <= 
     const int tiles = (n + 31) >> 5, stages = (tiles + TS - 1) / TS;
     const unsigned short* map = BIAS ? a.by_query + (size_t)(q0 >> 5) * a.NT * 1024 : nullptr;
     MapRegs mr, next;
-    int dead = 0;
+    RelAbout about = {0, 0};
     if (BIAS) {
-      fits = rel_plan_fits(a, &dead);
+      about = rel_about(a);
       if (mine) map_load(next, map, 0, lane);
       table_load(2 * D::STAGE, table, a, head, wave, waves, lane);
     }
@@ -538,12 +539,13 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, sizeof(T) == 2 && DH <= 
     RelKey key{0u, 0u};
     if (DROP) key = rel_key(a.rng, a.site);
     // stages that one of the workgroup's blocks needs, and of them the tiles that this wavefront's does
-    const Live live = live_start<BIAS>(reinterpret_cast<unsigned char*>(table + a.buckets + 1 + (a.buckets + 1 & 1)), a.live_query, dead, first >> 5, a.NT, wave, lane);
+    const Live live = live_start<BIAS>(reinterpret_cast<unsigned char*>(table + a.buckets + 1 + (a.buckets + 1 & 1)), a.live_query, about.dead, first >> 5, a.NT, wave, lane);
     auto tile_from = [&](int t) __attribute__((always_inline)) { return live_next(live.w, live.some, t, tiles); };
     auto stage_from = [&](int k) __attribute__((always_inline)) {
       const int t = live_next(live.all, live.some, k * TS, tiles);
       return t < tiles ? t / TS : stages;
     };
+    if (BIAS) fits = rel_plan_fits(a, about);
     int tn = mine && fits ? tile_from(0) : tiles;
     if (BIAS && tn > 0 && tn < tiles) map_load(next, map, tn, lane);
     for (int stage = 0, buf = 0; stage < stages; buf ^= 1) {
@@ -622,9 +624,10 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
   RelKey key{0u, 0u};
   if (DROP) key = rel_key(a.rng, a.site);
   const unsigned short* map = BIAS ? a.by_key + (size_t)(u0 >> 5) * a.NT * 1024 : nullptr;
-  int dead = 0;
+  RelAbout about = {0, 0};
+  if (BIAS) about = rel_about(a);
   const int end = min(all, (group + 1) * units);
-  if (BIAS && !rel_plan_fits(a, &dead)) {
+  if (BIAS && !rel_plan_fits(a, about)) {
     f32x16_t none[D::NM];
 #pragma unroll
     for (int mt = 0; mt < D::NM; ++mt) none[mt] = zero16();
@@ -638,7 +641,7 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
     }
     return;
   }
-  const Live live = live_start<BIAS>(reinterpret_cast<unsigned char*>(table + a.buckets + 1 + (a.buckets + 1 & 1)), a.live_key, dead, first >> 5, a.NT, wave, lane);
+  const Live live = live_start<BIAS>(reinterpret_cast<unsigned char*>(table + a.buckets + 1 + (a.buckets + 1 & 1)), a.live_key, about.dead, first >> 5, a.NT, wave, lane);
   int head = a.by_images.div(group * units), b = group * units - head * a.B;
   bool fresh = true;                 // the first image of its head here
   for (int unit = group * units; unit < end; ++unit, ++b) {

@@ -19,8 +19,8 @@ __global__ void __launch_bounds__(256) buckets_grid_kernel(int gw, int gh, int c
 }
 
 __global__ void __launch_bounds__(256) plan_maps_kernel(int T, int NT, int buckets, const int* __restrict__ bucket, unsigned short* __restrict__ by_query,
-                                                        unsigned short* __restrict__ by_key, int4* __restrict__ about) {
-  if (blockIdx.x == 0 && threadIdx.x == 0) *about = int4{0, kRelPlanMark, T, buckets};
+                                                        unsigned short* __restrict__ by_key, int* __restrict__ about) {
+  if (blockIdx.x == 0 && threadIdx.x == 0) about[0] = 0, about[1] = rel_plan_mark(T, buckets);
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < (size_t)NT * NT * 1024; i += (size_t)gridDim.x * 256) {
     const int block = (int)(i >> 10), t = block / NT * 32 + (int)(i >> 5 & 31), u = block % NT * 32 + (int)(i & 31);
     int k = buckets;
@@ -220,7 +220,7 @@ extern "C" int cnnk_rel_plan(int T, int buckets, const int* bucket, void* plan, 
   const int NT = (T + 31) / 32, places = NT * NT * 1024, per = ((places + kParts - 1) / kParts + 63) / 64 * 64;
   const size_t lds = (size_t)buckets * 4, blocks = ((size_t)places + 255) / 256;
   plan_maps_kernel<<<(unsigned)(blocks < 16384 ? blocks : 16384), 256, 0, st>>>(T, NT, buckets, bucket, (unsigned short*)(p + at.by_query), (unsigned short*)(p + at.by_key),
-                                                                                       (int4*)(p + at.about));
+                                                                                       (int*)(p + at.about));
   plan_live_kernel<<<dim3(NT, 2), 256, 0, st>>>(NT, buckets, (const unsigned short*)(p + at.by_query), (const unsigned short*)(p + at.by_key),
                                                (unsigned long long*)(p + at.live_query), (unsigned long long*)(p + at.live_key), (int*)(p + at.about));
   plan_order_kernel<<<NT * NT, 256, 0, st>>>(T, NT, buckets, bucket, (unsigned short*)(p + at.order), (unsigned*)(p + at.ends), runs);

@@ -6,6 +6,7 @@ read; cnnk_rng_advance moves its step on between training steps.  A bucket map (
 tensor; numbers outside 0 .. buckets - 1 mask a pair) becomes a plan once, with make_plan."""
 from __future__ import annotations
 import ctypes as C
+import functools
 import torch
 from .cnnk import lib, ptr, _check, F32, BF16  # noqa: F401
 
@@ -103,14 +104,20 @@ def rel_desc(B, T, heads, dh, dtype, buckets=0, p=0.0, site=0):
     return RelDesc(B, T, heads, dh, dtype, buckets, p, site)
 
 
-def _check_plan(d, plan):
-    if d.buckets > 0 and isinstance(plan, torch.Tensor) and plan.numel() * plan.element_size() < lib.cnnk_rel_plan_bytes(d.T, d.buckets):
+_plan_bytes = functools.lru_cache(4096)(cnnk_rel_plan_bytes)
+
+
+def _plan(d, plan):
+    """ptr() of a plan, which has to have the bytes that the call reads: a kernel cannot tell."""
+    if plan is None or isinstance(plan, int):
+        return plan
+    if plan.nbytes < _plan_bytes(d.T, d.buckets):
         raise ValueError("the plan is too small for %d tokens and %d buckets" % (d.T, d.buckets))
+    return plan.data_ptr()
 
 
 def cnnk_rel_attention_fwd(d, qkv, table, plan, lens, rng, o, stats=None, stream=0):
-    _check_plan(d, plan)
-    _check(lib.cnnk_rel_attention_fwd(C.byref(d), ptr(qkv), ptr(table), ptr(plan), ptr(lens), ptr(rng), ptr(o), ptr(stats), stream), "cnnk_rel_attention_fwd")
+    _check(lib.cnnk_rel_attention_fwd(C.byref(d), ptr(qkv), ptr(table), _plan(d, plan), ptr(lens), ptr(rng), ptr(o), ptr(stats), stream), "cnnk_rel_attention_fwd")
 
 
 def cnnk_rel_attention_workspace_bytes(d):
@@ -118,7 +125,6 @@ def cnnk_rel_attention_workspace_bytes(d):
 
 
 def cnnk_rel_attention_bwd(d, qkv, o, d_o, table, plan, lens, rng, stats, dqkv, dtable, ws, ws_bytes, stream=0):
-    _check_plan(d, plan)
-    _check(lib.cnnk_rel_attention_bwd(C.byref(d), ptr(qkv), ptr(o), ptr(d_o), ptr(table), ptr(plan), ptr(lens),
+    _check(lib.cnnk_rel_attention_bwd(C.byref(d), ptr(qkv), ptr(o), ptr(d_o), ptr(table), _plan(d, plan), ptr(lens),
                                       ptr(rng), ptr(stats), ptr(dqkv), ptr(dtable), ptr(ws), ws_bytes, stream),
            "cnnk_rel_attention_bwd")
