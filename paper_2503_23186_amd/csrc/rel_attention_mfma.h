@@ -235,12 +235,12 @@ struct Live {
   bool some;                         // blocks are left out
 };
 template <bool BIAS>
-__device__ __forceinline__ Live live_start(unsigned char* lds, const unsigned long long* p, int dead, int block0, int NT, int wave, int lane) {
+__device__ __forceinline__ Live live_start(unsigned char* lds, const unsigned long long* p, int dead, int block0, int NT, int wave, int waves, int lane) {
   unsigned long long* m = reinterpret_cast<unsigned long long*>(lds);
   Live l = {m + wave * 4, m + 32, BIAS && dead != 0};
   if (l.some) {
     if (threadIdx.x < 32) {
-      const unsigned long long v = block0 + (lane >> 2) < NT ? p[(size_t)block0 * 4 + lane] : 0;      // word lane % 4 of block lane / 4
+      const unsigned long long v = block0 + (lane >> 2) < NT && lane >> 2 < waves ? p[(size_t)block0 * 4 + lane] : 0;      // word lane % 4 of block lane / 4
       m[lane] = v;
       unsigned lo = (unsigned)v, hi = (unsigned)(v >> 32);
 #pragma unroll
@@ -410,7 +410,7 @@ __global__ void __launch_bounds__(512, sizeof(T) == 2 && DH <= 64 ? 4 : 2) rel_m
     RelKey key{0u, 0u};
     if (DROP) key = rel_key(a.rng, a.site);
     // stages that one of the workgroup's blocks needs, and of them the tiles that this wavefront's does
-    const Live live = live_start<BIAS>(reinterpret_cast<unsigned char*>(table + a.buckets + 1 + (a.buckets + 1 & 1)), a.live_query, about.dead, first >> 5, a.NT, wave, lane);
+    const Live live = live_start<BIAS>(reinterpret_cast<unsigned char*>(table + a.buckets + 1 + (a.buckets + 1 & 1)), a.live_query, about.dead, first >> 5, a.NT, wave, waves, lane);
     auto tile_from = [&](int t) __attribute__((always_inline)) { return live_next(live.w, live.some, t, tiles); };
     auto stage_from = [&](int k) __attribute__((always_inline)) {
       const int t = live_next(live.all, live.some, k * TS, tiles);
@@ -539,7 +539,7 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, sizeof(T) == 2 && DH <= 
     RelKey key{0u, 0u};
     if (DROP) key = rel_key(a.rng, a.site);
     // stages that one of the workgroup's blocks needs, and of them the tiles that this wavefront's does
-    const Live live = live_start<BIAS>(reinterpret_cast<unsigned char*>(table + a.buckets + 1 + (a.buckets + 1 & 1)), a.live_query, about.dead, first >> 5, a.NT, wave, lane);
+    const Live live = live_start<BIAS>(reinterpret_cast<unsigned char*>(table + a.buckets + 1 + (a.buckets + 1 & 1)), a.live_query, about.dead, first >> 5, a.NT, wave, waves, lane);
     auto tile_from = [&](int t) __attribute__((always_inline)) { return live_next(live.w, live.some, t, tiles); };
     auto stage_from = [&](int k) __attribute__((always_inline)) {
       const int t = live_next(live.all, live.some, k * TS, tiles);
@@ -641,7 +641,7 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mf
     }
     return;
   }
-  const Live live = live_start<BIAS>(reinterpret_cast<unsigned char*>(table + a.buckets + 1 + (a.buckets + 1 & 1)), a.live_key, about.dead, first >> 5, a.NT, wave, lane);
+  const Live live = live_start<BIAS>(reinterpret_cast<unsigned char*>(table + a.buckets + 1 + (a.buckets + 1 & 1)), a.live_key, about.dead, first >> 5, a.NT, wave, waves, lane);
   int head = a.by_images.div(group * units), b = group * units - head * a.B;
   bool fresh = true;                 // the first image of its head here
   for (int unit = group * units; unit < end; ++unit, ++b) {
