@@ -64,6 +64,24 @@ __device__ __forceinline__ int rel_block_runs(float* mine, const float4 (&s)[4],
   return __builtin_amdgcn_readlane((int)((ends >> 16) + __popc(ends & 0xffffu)), 63);
 }
 
+// How a walk is launched: the LDS of its workgroup (two stages of 4 KB a plane of 32 features and matrix, the head's column of the table, which blocks are there, in the walk for
+// dk and dv a stage's rows of statistics), its wavefronts, the parts of a (head, image) pair, and how many workgroups the device holds of the walk for dk and dv.
+constexpr int kLiveBytes = 9 * 32;
+constexpr size_t rel_stage_bytes(int dh) { return (size_t)(dh + 31) / 32 * 2 * 4096; }
+struct RelLaunch { size_t lds; int waves, parts, held; };
+static inline RelLaunch rel_launch(bool bf16, int dh, int NT, int buckets, bool backward) {
+  RelLaunch l;
+  l.lds = 2 * rel_stage_bytes(dh) + (buckets ? align_up((size_t)(buckets + 2) / 2 * 8 + kLiveBytes, 16) : 0) + (backward ? 2 * 3 * (bf16 ? 64 : 32) * 4 : 0);
+  // Eight wavefronts where a CU's LDS holds one workgroup (and the registers are there: the backward walks of heads of 128 take those of a SIMD for one wavefront), otherwise
+  // four (4096 tokens, 12 heads of 64, 16129 buckets: forward 241 us with four, 142 with eight, dq 280 and 179).
+  const bool alone = l.lds > 81920, one = backward && dh > 64;
+  const int most = alone && !one ? 8 : 4;
+  l.waves = NT < most ? NT : most;
+  l.parts = (NT + l.waves - 1) / l.waves;
+  l.held = alone || one ? 256 : 512;
+  return l;
+}
+
 // the first workgroup that has images of a head, and how many have them
 __host__ __device__ __forceinline__ int rel_first_group(int head, int B, int units) { return (int)((long long)head * B / units); }
 __host__ __device__ __forceinline__ int rel_groups(int head, int B, int units) {

@@ -126,12 +126,13 @@ RelArgs args_of(const cnnk_rel_desc* d, RelDrop dr, const float* table, const vo
 }
 // scratch of the backward pass: three floats for each row, and the sums of every pair, as often as a head's images lie in different workgroups
 size_t rows_bytes(const cnnk_rel_desc* d) { return align_up((size_t)d->B * d->heads * 3 * ((d->T + 63) / 64 * 64) * 4, 256); }
-// (head, image) pairs to a workgroup of the walk for dk and dv: as many as give every workgroup that the device holds (two to a CU, or one with heads of 128 or a
-// large table) the same number, so that there is one round of them and few sums to add up (64 images of 197 tokens, 12 heads of 64: the walk 77 us, 87 with one pair to a
-// workgroup).
+// (head, image) pairs to a workgroup of the walk for dk and dv: as many as give every workgroup that the device holds (two to a CU, or one) the same number, so that there
+// is one round of them and few sums to add up (64 images of 197 tokens, 12 heads of 64: the walk 77 us, 87 with one pair to a workgroup; 16 images of 4096 tokens, 3 heads
+// of 64, 16129 buckets: backward 1990 us with the three that fill the device, 2440 with six; 9 images of 2601 tokens, 12 heads of 32 the other way, 2038 with five, 1957 with
+// nine, whose sums lie in two slots instead of three).
 int units_of(const cnnk_rel_desc* d) {
-  const long NT = (d->T + 31) / 32, held = d->dh == 128 || d->buckets > 10000 ? 256 : 512;
-  const long units = ((long)d->B * d->heads * ((NT + 3) / 4) + held - 1) / held;
+  const RelLaunch l = rel_launch(d->dtype == CNNK_BF16, d->dh, (d->T + 31) / 32, d->buckets, true);
+  const long units = ((long)d->B * d->heads * l.parts + l.held - 1) / l.held;
   return (int)(units < d->B ? units : d->B);
 }
 size_t pairs_bytes(const cnnk_rel_desc* d) {

@@ -228,7 +228,6 @@ __device__ __forceinline__ f32x16_t score_tile(const unsigned char* m, const typ
 
 // ---- blocks that are not all masked ----------------------------------------------------------------------------------------------
 // Which blocks of the other side a wavefront's block, and any of its workgroup's, has pairs with: in LDS, since few maps leave any out.
-constexpr int kLiveBytes = 9 * 32;
 struct Live {
   const unsigned long long* w;       // bits of the wavefront's block
   const unsigned long long* all;     // of the workgroup's together
@@ -785,18 +784,12 @@ template <typename Kern> int allow_lds(Kern kern, size_t bytes) {      // more t
   if (bytes <= 65536) return CNNK_OK;
   return hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess ? CNNK_OK : CNNK_ERR_HIP;
 }
-size_t table_bytes(const RelArgs& a) { return a.buckets ? align_up((size_t)(a.buckets + 2) / 2 * 8 + kLiveBytes, 16) : 0; }      // and what is behind it
-
-// A workgroup's wavefronts: eight where the table takes so much LDS that a CU holds one workgroup (and the registers are there), otherwise four
-// (4096 tokens, 12 heads of 64, 16129 buckets: forward 241 us with four, 142 with eight, dq 280 and 179).
-int waves_of(const RelArgs& a, size_t lds, bool eight) {
-  const int most = eight && lds > 81920 ? 8 : 4;
-  return a.NT < most ? a.NT : most;
-}
 template <typename T, int DH, bool BIAS, bool DROP>
 int fwd_launch(const RelArgs& a, const T* qkv, T* o, float* stats, hipStream_t st) {
-  const size_t lds = 2 * Dim<T, DH>::STAGE + table_bytes(a);
-  const int waves = waves_of(a, lds, true), parts = (a.NT + waves - 1) / waves, pairs = a.B * a.heads;
+  static_assert(Dim<T, DH>::STAGE == rel_stage_bytes(DH), "");
+  const RelLaunch l = rel_launch(sizeof(T) == 2, DH, a.NT, a.buckets, false);
+  const size_t lds = l.lds;
+  const int waves = l.waves, parts = l.parts, pairs = a.B * a.heads;
   const auto kern = rel_mfma_fwd_kernel<T, DH, BIAS, DROP>;
   if (allow_lds(kern, lds) != CNNK_OK) return CNNK_ERR_HIP;
   kern<<<grid_of(pairs, parts), 64 * waves, lds, st>>>(a, qkv, o, stats, fast_div(parts));
@@ -804,8 +797,9 @@ int fwd_launch(const RelArgs& a, const T* qkv, T* o, float* stats, hipStream_t s
 }
 template <typename T, int DH, bool BIAS, bool DROP>
 int bwd_launch(const RelArgs& a, const T* qkv, const T* o, const T* d_o, const float* stats, T* dqkv, float* rows, float* pairs, int units, bool* runs, hipStream_t st) {
-  const size_t lds = 2 * Dim<T, DH>::STAGE + table_bytes(a), lds_kv = lds + 2 * 3 * Dim<T, DH>::KB * 4;
-  const int waves = waves_of(a, lds_kv, DH <= 64), parts = (a.NT + waves - 1) / waves, heads = a.B * a.heads;
+  const RelLaunch l = rel_launch(sizeof(T) == 2, DH, a.NT, a.buckets, true);
+  const size_t lds_kv = l.lds, lds = lds_kv - 2 * 3 * Dim<T, DH>::KB * 4;
+  const int waves = l.waves, parts = l.parts, heads = a.B * a.heads;
   // The walk itself adds up a block's runs (which makes it longer) where a single image's sums of pairs are more than the caches hold, so that a kernel behind it would
   // read them from memory, and where the workgroup has a CU's LDS to itself.  us of the walk, the runs and the gather, 12 heads of 64 bf16, pairs written | runs written:
   // 1024 tokens (a table for 4096) 84 | 101, 3136 tokens 401 | 340, 4096 tokens 619 | 436, 4096 tokens in windows of 15 x 15 150 | 143.  With more images it would

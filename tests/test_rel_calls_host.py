@@ -15,3 +15,22 @@ def test_a_plan_tensor_of_fewer_bytes_is_refused():
             rel.cnnk_rel_attention_fwd(d, A, A, plan, None, None, A, A)
         with pytest.raises(ValueError):
             rel.cnnk_rel_attention_bwd(d, A, A, A, A, plan, None, None, A, A, A, A, 1 << 40)
+
+
+@pytest.mark.parametrize("B,T,heads,dh,dtype,buckets,units", [
+    (64, 197, 12, 64, cnnk.BF16, 732, 3),           # 7 blocks, 2 parts of four wavefronts, two workgroups to a CU: 64 * 12 * 2 / 512
+    (16, 4096, 3, 64, cnnk.BF16, 16129, 3),         # LDS for one workgroup to a CU, of eight wavefronts: 128 / 8 = 16 parts, 48 * 16 / 256
+    (4, 4096, 12, 64, cnnk.BF16, 16129, 3),
+    (7, 4096, 12, 64, cnnk.BF16, 16129, 6),         # 5.25
+    (9, 2601, 12, 32, cnnk.BF16, 10201, 5),         # 58 KB: two to a CU, of four: 82 blocks, 21 parts, 108 * 21 / 512
+    (8, 4096, 2, 16, cnnk.BF16, 15000, 1),          # 77 KB: 16 * 32 / 512
+    (8, 4096, 2, 16, cnnk.F32, 16382, 1),           # 83 KB, one to a CU: 16 * 16 / 256
+    (7, 2601, 12, 128, cnnk.BF16, 10201, 7),        # one workgroup of four to a CU: 84 * 21 / 256 = 6.9
+    (9, 200, 12, 64, cnnk.F32, 16382, 1),           # seven blocks: one part of seven wavefronts, 108 / 256
+])
+def test_images_of_a_workgroup_fill_the_device_that_the_launch_meets(B, T, heads, dh, dtype, buckets, units):
+    """A head's images lie in 1 + (B - 1) / units workgroups, rounded up, at most; the workspace has the sums of each, in blocks of 4 KB, and three floats for each row."""
+    blocks, rows = (T + 31) // 32, (B * heads * 3 * ((T + 63) // 64 * 64) * 4 + 255) // 256 * 256
+    need = rel.cnnk_rel_attention_workspace_bytes(rel.rel_desc(B, T, heads, dh, dtype, buckets))
+    slot = heads * blocks * blocks * 4096
+    assert (need - rows) % slot == 0 and (need - rows) // slot == 1 + (B - 1 + units - 1) // units
