@@ -135,12 +135,19 @@ int units_of(const cnnk_rel_desc* d) {
   const long units = ((long)d->B * d->heads * l.parts + l.held - 1) / l.held;
   return (int)(units < d->B ? units : d->B);
 }
+// A head's images start at a multiple of g, the greatest divisor of B and units, behind a workgroup's start: units - g at most, so that they lie in (units - g + B) / units
+// workgroups, rounded up.
 size_t pairs_bytes(const cnnk_rel_desc* d) {
   const size_t NT = (d->T + 31) / 32;
   const int units = units_of(d);
-  return (size_t)((d->B + units - 2) / units + 1) * d->heads * NT * NT * 4096;
+  int g = d->B;
+  for (int r = units; r;) {
+    const int next = g % r;
+    g = r, r = next;
+  }
+  return (size_t)(1 + (d->B - g + units - 1) / units) * d->heads * NT * NT * 4096;
 }
-
+size_t workspace_bytes(const cnnk_rel_desc* d, bool dtable) { return rows_bytes(d) + (d->buckets && dtable ? pairs_bytes(d) : 0); }
 }  // namespace
 
 extern "C" int cnnk_rel_attention_fwd(const cnnk_rel_desc* d, const void* qkv, const float* table, const void* plan, const int* lens, const unsigned long long* rng,
@@ -160,7 +167,7 @@ extern "C" int cnnk_rel_attention_fwd(const cnnk_rel_desc* d, const void* qkv, c
 extern "C" size_t cnnk_rel_attention_workspace_bytes(const cnnk_rel_desc* d) {
   RelDrop dr;
   if (check(d, &dr) != CNNK_OK) return 0;
-  return rows_bytes(d) + (d->buckets ? pairs_bytes(d) : 0);
+  return workspace_bytes(d, true);
 }
 
 extern "C" int cnnk_rel_attention_bwd(const cnnk_rel_desc* d, const void* qkv, const void* o, const void* d_o, const float* table, const void* plan,
@@ -170,7 +177,7 @@ extern "C" int cnnk_rel_attention_bwd(const cnnk_rel_desc* d, const void* qkv, c
   const int rc = check(d, &dr);
   if (rc != CNNK_OK) return rc;
   if (!qkv || !o || !d_o || !stats || !dqkv || (d->buckets && (!table || !plan)) || (dr.q && !rng)) return CNNK_ERR_NULL;
-  if (!ws || ws_bytes < cnnk_rel_attention_workspace_bytes(d)) return CNNK_ERR_WORKSPACE;
+  if (!ws || ws_bytes < workspace_bytes(d, dtable != nullptr)) return CNNK_ERR_WORKSPACE;
   if (!rel_aligned(qkv, 16) || !rel_aligned(o, 16) || !rel_aligned(d_o, 16) || !rel_aligned(stats, 8) || !rel_aligned(table, 4) ||
       !rel_aligned(plan, 256) || !rel_aligned(lens, 4) || !rel_aligned(rng, 8) || !rel_aligned(dqkv, 16) || !rel_aligned(dtable, 4) || !rel_aligned(ws, 16))
     return CNNK_ERR_UNSUPPORTED;

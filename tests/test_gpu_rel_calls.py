@@ -121,6 +121,42 @@ def test_a_long_image_with_a_plan_of_another_map(K, T, n):
     assert torch.isnan(dq).all() and torch.isnan(dt).all() and (ws[:512] == 77).all() and (ws[512 + need:] == 77).all()
 
 
+# ---- workspaces ------------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,B,T,heads,dh,buckets", [("bf16", 8, 300, 60, 16, 12000), ("bf16", 95, 40, 12, 64, 0), ("bf16", 64, 50, 24, 32, 0), ("f32", 7, 260, 60, 32, 0), ("bf16", 7, 2050, 12, 16, 0)])
+def test_sums_stay_in_the_workspace(K, dtype, B, T, heads, dh, buckets):
+    """Three images to a workgroup, in batches that three does not divide, so that heads begin everywhere in one: nothing behind the workspace is written, and with dtable = NULL
+    nothing behind the rows; the table's gradient is that of one image after the other.
+
+    A bucket has M = T * T / 91 * B terms of either sign, sums of k of them are about sqrt(k) of one, and adding to one rounds by 2^-24 of it at most.  The roundings of all
+    M additions, independent, are together 2^-24 sqrt(1 + 2 + .. + M) = 2^-24 M / sqrt(2) of a term, 2^-24 sqrt(M / 2) of the sum; there are two such sums, and a factor 2 is for
+    terms of unlike size."""
+    n = buckets or 91
+    g = torch.Generator(device=DEV).manual_seed(B)
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    rand = lambda *s: torch.randn(*s, generator=g, device=DEV)
+    qkv, do, table = rand(B, T, 3 * heads * dh).to(t), rand(B, T, heads * dh).to(t), rand(n, heads)
+    plan = K.make_plan(torch.randint(-1, 91, (T, T), generator=g, device=DEV, dtype=torch.int32), n)
+    desc = lambda b, k=n: K.rel_desc(b, T, heads, dh, K.BF16 if dtype == "bf16" else K.F32, k, 0.0, 0)
+
+    def run(b, q, d, dt, need):
+        o, st, dq = torch.empty_like(d), torch.empty(b, heads, T, 2, device=DEV), torch.empty_like(q)
+        ws = torch.full((need + 4096,), 77, dtype=torch.uint8, device=DEV)
+        K.cnnk_rel_attention_fwd(desc(b), q, table, plan, None, None, o, st)
+        K.cnnk_rel_attention_bwd(desc(b), q, o, d, table, plan, None, None, st, dq, dt, ws, need)
+        assert (ws[need:] == 77).all()
+        return dq
+
+    dt, one, want = torch.empty_like(table), torch.empty_like(table), torch.zeros_like(table, dtype=torch.float64)
+    dq = run(B, qkv, do, dt, K.cnnk_rel_attention_workspace_bytes(desc(B)))
+    assert torch.equal(run(B, qkv, do, None, K.cnnk_rel_attention_workspace_bytes(desc(B, 0))), dq)
+    for b in range(B):
+        alone = run(1, qkv[b:b + 1], do[b:b + 1], one, K.cnnk_rel_attention_workspace_bytes(desc(1)))
+        assert torch.equal(alone[0], dq[b])
+        want += one.double()
+    assert float((dt.double() - want).norm() / want.norm()) <= 2.0 * 2.0 ** -24 * np.sqrt(T * T / 91 * B)      # sqrt(2) sums, times 2
+
+
 # ---- addresses -------------------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype,T", [("bf16", 45), ("f32", 130)])
