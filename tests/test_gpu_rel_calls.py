@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from test_gpu_rel import DEV, Case, map_of
+from test_gpu_rel_block import reference64
 
 pytestmark = pytest.mark.gpu
 
@@ -155,6 +156,50 @@ def test_sums_stay_in_the_workspace(K, dtype, B, T, heads, dh, buckets):
         assert torch.equal(alone[0], dq[b])
         want += one.double()
     assert float((dt.double() - want).norm() / want.norm()) <= 2.0 * 2.0 ** -24 * np.sqrt(T * T / 91 * B)      # sqrt(2) sums, times 2
+
+
+@pytest.mark.parametrize("dtype,B,T,heads,dh", [("bf16", 20, 70, 56, 16), ("bf16", 11, 130, 52, 64), ("bf16", 11, 100, 60, 32), ("bf16", 7, 65, 80, 128), ("f32", 20, 70, 56, 64),
+                                                ("f32", 11, 130, 52, 32), ("f32", 7, 65, 80, 128)])
+@pytest.mark.parametrize("kind,p,ragged", [("grid", 0.1, False), ("random", 0.2, True), ("grid", 0.0, True)])
+def test_workgroups_that_go_from_head_to_head(K, dtype, B, T, heads, dh, kind, p, ragged):
+    """Two or three images to a workgroup, in batches that these do not divide: in the walk for dk and dv a workgroup goes on to the next head, loads its column of the table and adds
+    up dx of several images that have tokens.  Every element against the oracle; padded batches with empty images at the ends of a workgroup's."""
+    bucket, n = map_of(kind, T)
+    lens = [(0, T, T - 1, 33, T // 2, 1, T, 0, 64)[i % 9] for i in range(B)] if ragged else None
+    Case(K, dtype, B, T, heads, dh, bucket, n, p, lens=lens, past=np.nan).check()
+
+
+# ---- long images ---------------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,T,heads,dh,buckets", [(t,) + c for t in ("f32", "bf16") for c in ((300, 2, 64, 16382), (2049, 1, 32, 3), (4100, 1, 64, 16129), (8192, 1, 16, 40))] +
+                         [("f32", 16384, 1, 16, 0), ("f32", 5000, 1, 128, 0)])
+def test_long_images_to_fp32(K, dtype, T, heads, dh, buckets):
+    """Norm of the error over the norm of the result, fp32 storage, and the table's gradient, an fp32 sum, with either.  Terms of either sign: a sum of k terms is about sqrt(k) of
+    one, so that the roundings of T additions, independent, are 2^-24 sqrt(T / 2) of the sum, those of a score's dh products 2^-24 sqrt(dh / 2).  A probability has besides the
+    rounding of the exponent, a number below 32 (16 2^-24), of the difference in front of it, below 16 (8 2^-24), of the logarithm of the sum (8 2^-24), and of the exponential and
+    the products around it (fewer than 16 of 2^-24): e = 2^-24 (sqrt(T / 2) + sqrt(dh / 2) + 48).  dx has the errors of a probability and of dP: 2 e for the gradients.  A
+    bucket's sum has chains of 32 pairs of a block, then of its runs: 64 or more threads share more than 4096, so that sqrt(T / 2) is not passed."""
+    gen = torch.Generator(device=DEV).manual_seed(T + dh)
+    t = torch.bfloat16 if dtype == "bf16" else torch.float32
+    rand = lambda *s: torch.randn(*s, generator=gen, device=DEV)
+    qkv, g = rand(T, 3 * heads * dh).to(t), rand(T, heads * dh).to(t)
+    table = plan = bucket = dt = None
+    if buckets:
+        table = rand(buckets, heads)
+        bucket = torch.randint(-1, buckets, (T, T), generator=gen, device=DEV, dtype=torch.int32)
+        plan, dt = K.make_plan(bucket, buckets), torch.full_like(table, 7.0)
+    d = K.rel_desc(1, T, heads, dh, K.BF16 if dtype == "bf16" else K.F32, buckets, 0.0, 0)
+    o, stats, dq = torch.full((T, heads * dh), 7.0, device=DEV, dtype=t), torch.empty(1, heads, T, 2, device=DEV), torch.full_like(qkv, 7.0)
+    ws = torch.empty(K.cnnk_rel_attention_workspace_bytes(d), dtype=torch.uint8, device=DEV)
+    K.cnnk_rel_attention_fwd(d, qkv, table, plan, None, None, o, stats)
+    K.cnnk_rel_attention_bwd(d, qkv, o, g, table, plan, None, None, stats, dq, dt, ws, ws.numel())
+    wo, wd, wt = reference64(qkv, heads, dh, table, bucket, g)
+    off = lambda a, b: float((a.double() - b).norm() / b.norm())
+    e = 2.0 ** -24 * ((T / 2) ** 0.5 + (dh / 2) ** 0.5 + 48)
+    if dtype == "f32":
+        assert off(o, wo) <= e and off(dq, wd) <= 2 * e, (off(o, wo), off(dq, wd), e)
+    if buckets:
+        assert off(dt, wt) <= 2 * e, (off(dt, wt), e)
 
 
 # ---- addresses -------------------------------------------------------------------------------------------------------------------
