@@ -370,6 +370,7 @@ template <int N> __device__ __forceinline__ void scale_rows(f32x16_t* acc, float
 __device__ __forceinline__ int key_of(int i, int h) { return (i >> 2) * 8 + h * 4 + (i & 3); }
 
 // ---- forward ---------------------------------------------------------------------------------------------------------------
+// 128 registers leave four wavefronts to a SIMD (bf16, heads of up to 64); with heads of 64, bias and dropout one more is spilled (8 bytes of scratch).
 template <typename T, int DH, bool BIAS, bool DROP>
 __global__ void __launch_bounds__(512, sizeof(T) == 2 && DH <= 64 ? 4 : 2) rel_mfma_fwd_kernel(RelArgs a, const T* __restrict__ qkv, T* __restrict__ o,
                                                                              float* __restrict__ stats, FastDiv parts) {
@@ -604,6 +605,8 @@ __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, sizeof(T) == 2 && DH <= 
 // dx of its keys to pairs [slot][heads][NT keys][NT queries][4][64][4], the slot being the workgroup's number among those that have images of the head: a
 // tile's sums so far come in while its scores are formed; they are a wavefront's own, in the caches, so the sum over images has one order and needs
 // no atomics.
+// Registers are short: with bias and dropout 90 to 100 scalar ones lie in lanes of vector registers (about 15 reads a tile, 116 an image), and fp32 with heads of 64 has two
+// vector registers in scratch (12 bytes).  Heads of 128 take 400 and more, one wavefront to a SIMD.
 template <typename T, int DH, bool BIAS, bool DROP, bool RUNS>
 __global__ void __launch_bounds__(DH <= 64 ? 512 : 256, DH <= 64 ? 2 : 1) rel_mfma_dkv_kernel(RelArgs a, const T* __restrict__ qkv, const T* __restrict__ d_o,
                                                                              const float* __restrict__ rows, T* __restrict__ dqkv, float* pairs, FastDiv parts,
