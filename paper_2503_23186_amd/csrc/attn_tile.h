@@ -1,4 +1,4 @@
-// Pieces of the attention kernels on the matrix cores (v_mfma_f32_32x32x16_bf16), shared by vit_attention_mfma.hip and rel_attention_mfma.hip:
+// Pieces of the attention kernels on the matrix cores (v_mfma_f32_32x32x16_bf16), shared by vit_attention_mfma.hip and rel_attention_mfma.h:
 // the LDS layout of a matrix with a token a row, reads of it as operands, score tiles, stores.
 // Planes of 32 features with 64-byte rows whose 16-byte chunks are XOR-swizzled by row bits 2-3; NK = features / 16, NM = planes.
 #pragma once

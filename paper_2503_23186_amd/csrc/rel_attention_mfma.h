@@ -27,6 +27,7 @@
 
 namespace {
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
+// Online softmax (M. Milakov, N. Gimelshein, 2018) with a reference that is raised lazily (the conditional rescaling that T. Dao presented in 2025).
 // Probabilities are summed as 2^((x - m) log2 e - down), where m is a reference that a row's largest score so far passes by at most `slack`, and 2^down is T times
 // 2^(slack log2 e): sums over T keys stay below the largest value.  A reference that is raised lazily saves rescaling; fp32 storage, whose time the
 // products take, has none of it, since the bits of `down` are missing in the exponent's fraction.
@@ -146,9 +147,9 @@ template <int DH> struct Dim<float, DH> {
   }
 };
 
-// acc += M^T x in the backward pass.  bf16: x is rounded to 2^-8, as is the result.  Over many pairs that is one more rounding of the result's own size (1.43 times its error
-// alone); with a few tokens it is up to 1.56 times, so images of one tile add a product with what the rounding took off (1.05 to 1.3
-// times; both walks together 21.8 -> 23.0 us at 64 images of 25 tokens and 12 heads of 64, where starting takes most of it).
+// acc += M^T x in the backward pass.  bf16: x is rounded to 2^-8, as is the result.  Two independent roundings of one size have sqrt(2) times the error of one; that is what operands
+// in bf16 cost, and stays (1.43 measured over many pairs, from 33 tokens on).  Images of one tile were above it, up to 1.56: they add a product with what the rounding took off (1.05
+// to 1.3; both walks together 21.8 -> 23.0 us at 64 images of 25 tokens and 12 heads of 64, where starting takes most of it).
 template <typename T, int DH> __device__ __forceinline__ void tn_bwd(const unsigned char* m, const f32x16_t& x, f32x16_t* acc, int lane, bool one_tile) {
   Dim<T, DH>::tn(m, x, acc, lane);
   if (sizeof(T) == 2 && one_tile) {
