@@ -66,8 +66,9 @@ int cnnk_rel_plan(int T, int buckets, const int* bucket, void* plan, void* ws, s
  * ones (taken as 0 .. T).  A row that sees no key, and every row past the image's tokens, has o = 0 and no part in any gradient;
  * what qkv and d_o hold past an image's tokens, NaN too, is of no account.  Scores of -infinity from the table mask as well; the
  * lowest finite value does not (a row of nothing else is shared out evenly).  Features of an image's own tokens must be finite:
- * masked pairs are computed and left out.  What is not (a NaN or an infinity in them or in the table, a score that overflows) is handed
- * on as NaN: to the rows that see it, their statistics and all gradients they take part in, and maybe to other rows of that image and head.
+ * masked pairs are computed and left out.  A score that is NaN or +infinity (from a feature or the table that is not finite, or by overflow) is
+ * handed on as NaN: to the rows that see it, their statistics and all gradients they take part in, and maybe to other rows of that image and
+ * head; a score of -infinity masks its pair wherever it comes from.
  * table [buckets][heads] float; buckets = 0: no bias, table and plan are not read.
  * Dropout: query t, key u of (image b, head h) has half u % 2 of word t % 4 of F(u / 2, t / 4, b * heads + h, 2).
  * Training: stats [B][heads][T][2] receives a reference near each row's largest x and the logarithm of

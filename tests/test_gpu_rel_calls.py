@@ -3,8 +3,10 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import rel as R
 from test_gpu_rel import DEV, Case, map_of
 from test_gpu_rel_block import reference64
+from util import host
 
 pytestmark = pytest.mark.gpu
 
@@ -52,6 +54,27 @@ def test_what_is_not_finite_is_handed_on(K, dtype, T, p, where):
     for a, b, k in ((o, clean[0], 1), (dq, clean[2], 3)):
         a, b = keep(a, k), keep(b, k)
         assert torch.equal(a[0::2], b[0::2]) and torch.equal(a[:, :, :, 1], b[:, :, :, 1])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [17, 130])
+def test_scores_that_overflow_downwards_mask(K, dtype, T):
+    """-infinity: one key of a row, then all of them."""
+    B, heads, dh = 2, 2, 64
+    bucket, n = map_of("grid", T)
+    c = Case(K, dtype, B, T, heads, dh, bucket, n, 0.0)
+    q = c.gq.view(B, T, 3, heads, dh)
+    q[0, 3, 0, 0], q[0, 3, 0, 0, 0] = 0.0, 1e38
+    q[0, :, 1, 0, 0] = 0.0
+    q[0, 5, 1, 0, 0] = -100.0
+    o, m = c.fwd()
+    masked = np.array(bucket)
+    masked[3, 5] = -1
+    want = R.attention(host(q).reshape(B, T, -1) * 1.0, heads, c.table, masked)
+    assert np.abs(host(o)[0, 3, :dh] - want["o"][0, 3, :dh]).max() <= (2.0 ** -7 if dtype == "bf16" else 2.0 ** -18) * np.abs(want["bound_o"][0, 3, :dh]).max()
+    q[0, :, 1, 0, 0] = -100.0
+    o, m = c.fwd()
+    assert (o[0, 3, :dh] == 0).all() and m[0, 0, 3].tolist() == [-np.inf, 0.0] and torch.isfinite(o).all()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
