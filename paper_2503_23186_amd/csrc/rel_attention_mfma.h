@@ -784,9 +784,10 @@ int grid_of(int groups, int parts) {
   const int whole = whole_groups(groups, parts);
   return (whole * parts + last_share(groups, whole, parts)) * 8;
 }
-template <typename Kern> int allow_lds(Kern kern, size_t bytes) {      // more than 64 KB has to be asked for, on the device that is current
+// More than 64 KB has to be asked for, on the device that is current: always a CU's 160 KB, so that no call takes back what another host thread's asked for.
+template <typename Kern> int allow_lds(Kern kern, size_t bytes) {
   if (bytes <= 65536) return CNNK_OK;
-  return hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess ? CNNK_OK : CNNK_ERR_HIP;
+  return hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) == hipSuccess ? CNNK_OK : CNNK_ERR_HIP;
 }
 template <typename T, int DH, bool BIAS, bool DROP>
 int fwd_launch(const RelArgs& a, const T* qkv, T* o, float* stats, hipStream_t st) {

@@ -1,4 +1,6 @@
 """Calls of include/cnnk_rel.h that its documentation allows and where one value, address or size decides: against oracle/rel.py in float64."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -223,6 +225,101 @@ def test_long_images_to_fp32(K, dtype, T, heads, dh, buckets):
         assert off(o, wo) <= e and off(dq, wd) <= 2 * e, (off(o, wo), off(dq, wd), e)
     if buckets:
         assert off(dt, wt) <= 2 * e, (off(dt, wt), e)
+
+
+# ---- host threads --------------------------------------------------------------------------------------------------------------------
+
+def test_calls_from_host_threads_at_once(K):
+    """Tables that take different shares of more than 64 KB of LDS, each from a thread and on a stream of its own: every call is taken, the results are those of calls alone."""
+    def case(n):
+        T, heads, dh = 260, 2, 64
+        g = torch.Generator(device=DEV).manual_seed(n)
+        rand = lambda *s: torch.randn(*s, generator=g, device=DEV)
+        qkv, do, table = rand(2, T, 3 * heads * dh).bfloat16(), rand(2, T, heads * dh).bfloat16(), rand(n, heads)
+        plan = K.make_plan(torch.randint(-1, n, (T, T), generator=g, device=DEV, dtype=torch.int32), n)
+        d = K.rel_desc(2, T, heads, dh, K.BF16, n, 0.0, 0)
+        o, st, dq, dt = torch.empty_like(do), torch.empty(2, heads, T, 2, device=DEV), torch.empty_like(qkv), torch.empty_like(table)
+        ws = torch.empty(K.cnnk_rel_attention_workspace_bytes(d), dtype=torch.uint8, device=DEV)
+
+        def step(stream):
+            K.cnnk_rel_attention_fwd(d, qkv, table, plan, None, None, o, st, stream)
+            K.cnnk_rel_attention_bwd(d, qkv, o, do, table, plan, None, None, st, dq, dt, ws, ws.numel(), stream)
+        return step, (o, st, dq, dt)
+
+    cases, streams, failed = [case(n) for n in (9000, 12000, 16382)], [torch.cuda.Stream() for _ in range(3)], []
+    want = []
+    for step, out in cases:
+        step(0)
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in out])
+        for t in out:
+            t.zero_()
+    torch.cuda.synchronize()
+
+    def work(step, stream):
+        try:
+            for _ in range(200):
+                step(stream)
+        except Exception as e:
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=(c[0], s.cuda_stream)) for c, s in zip(cases, streams)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not failed, failed
+    for (_, out), w in zip(cases, want):
+        assert all(torch.equal(a, b) for a, b in zip(out, w))
+
+
+# ---- the largest and the smallest -----------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("B,heads,buckets", [(8388599, 1, 0), (1, 1, 1), (128, 65535, 0), (65536, 100, 1)])
+def test_images_of_one_token(K, B, heads, buckets):
+    """As many as a launch can have: the output is v, its gradient d_o, bit for bit; q, k and the table have none (dP is delta, but for the rounding of two sums of 16
+    products: 24 2^-24 of their terms' sizes, 16 * 4.5^2 at most, times |k| / 4; for the table the sum of B such numbers)."""
+    dh, g = 16, torch.Generator(device=DEV).manual_seed(2)
+    qkv, do = torch.randn(B, 1, 3 * heads * dh, generator=g, device=DEV, dtype=torch.float32).bfloat16().clamp_(-4.5, 4.5), torch.randn(B, 1, heads * dh, generator=g, device=DEV).bfloat16().clamp_(-4.5, 4.5)
+    d = K.rel_desc(B, 1, heads, dh, K.BF16, buckets, 0.0, 0)
+    table = plan = dt = None
+    if buckets:
+        table, plan, dt = torch.randn(1, heads, generator=g, device=DEV), K.make_plan(torch.zeros(1, 1, dtype=torch.int32, device=DEV), 1), torch.full((1, heads), 7.0, device=DEV)
+    o, st, dq = torch.zeros_like(do), torch.zeros(B, heads, 1, 2, device=DEV), torch.full_like(qkv, 7.0)
+    ws = torch.empty(K.cnnk_rel_attention_workspace_bytes(d), dtype=torch.uint8, device=DEV)
+    K.cnnk_rel_attention_fwd(d, qkv, table, plan, None, None, o, st)
+    K.cnnk_rel_attention_bwd(d, qkv, o, do, table, plan, None, None, st, dq, dt, ws, ws.numel())
+    w = heads * dh
+    assert torch.equal(o, qkv[..., 2 * w:]) and torch.equal(dq[..., 2 * w:], do)
+    one = 24 * 2.0 ** -24 * 2 * 16 * 4.5 ** 2
+    assert float(dq[..., :2 * w].abs().max()) <= one * 4.5 / 4 * 1.01
+    if buckets:
+        assert float(dt.abs().max()) <= one * B
+
+
+def test_as_many_heads_as_there_are(K):
+    """65535 heads, with a bias: every one by the formula in 64 bits."""
+    B, T, heads, dh, n = 3, 3, 65535, 16, 4
+    g = torch.Generator(device=DEV).manual_seed(9)
+    rand = lambda *s: torch.randn(*s, generator=g, device=DEV)
+    qkv, do, table = rand(B, T, 3 * heads * dh), rand(B, T, heads * dh), rand(n, heads)
+    bucket = torch.tensor([[0, 1, -1], [2, 3, 0], [1, -1, 2]], dtype=torch.int32, device=DEV)
+    d, plan = K.rel_desc(B, T, heads, dh, K.F32, n, 0.0, 0), K.make_plan(bucket, n)
+    o, st, dq, dt = torch.zeros_like(do), torch.zeros(B, heads, T, 2, device=DEV), torch.full_like(qkv, 7.0), torch.full_like(table, 7.0)
+    ws = torch.empty(K.cnnk_rel_attention_workspace_bytes(d), dtype=torch.uint8, device=DEV)
+    K.cnnk_rel_attention_fwd(d, qkv, table, plan, None, None, o, st)
+    K.cnnk_rel_attention_bwd(d, qkv, o, do, table, plan, None, None, st, dq, dt, ws, ws.numel())
+    q, k, v = (x.requires_grad_() for x in qkv.double().view(B, T, 3, heads, dh).permute(2, 0, 3, 1, 4).contiguous().unbind(0))
+    w = table.double().requires_grad_()
+    x = (q[..., :, None, :] * k[..., None, :, :]).sum(-1) / 4 + w[bucket.long().clamp(min=0)].permute(2, 0, 1)
+    y = (torch.softmax(x.masked_fill(bucket < 0, -1e300), -1)[..., None] * v[..., None, :, :]).sum(-2)
+    y.backward(do.double().view(B, T, heads, dh).transpose(1, 2))
+    off = lambda a, b: float((a.double() - b).norm() / b.norm())
+    e = 2.0 ** -24 * 48                          # as in test_long_images_to_fp32, whose sums are longer
+    assert off(o.view(B, T, heads, dh), y.detach().transpose(1, 2)) <= e and off(dt, w.grad) <= 2 * e
+    for i, t in enumerate((q, k, v)):
+        assert off(dq.view(B, T, 3, heads, dh)[:, :, i], t.grad.transpose(1, 2)) <= 2 * e
 
 
 # ---- addresses -------------------------------------------------------------------------------------------------------------------
