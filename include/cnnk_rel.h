@@ -40,7 +40,7 @@ int cnnk_dropout_fwd(const cnnk_dropout_desc* d, const void* z, const float* bia
                      const unsigned long long* rng, void* y, void* stream);
 
 /* dz = keep * dy / (1 - p); dbias[c] = sum_r dz[r, c] of the unrounded values, if dbias is not NULL (the gradient of res is dy
- * itself).  dz may alias dy.  ws is needed with dbias only. */
+ * itself).  dz may alias dy.  ws is needed with dbias only, C is 2^30 at most then. */
 size_t cnnk_dropout_workspace_bytes(const cnnk_dropout_desc* d);
 int cnnk_dropout_bwd(const cnnk_dropout_desc* d, const void* dy, const unsigned long long* rng, void* dz, float* dbias, void* ws,
                      size_t ws_bytes, void* stream);

@@ -117,6 +117,7 @@ int check(const cnnk_dropout_desc* d, RelDrop* dr) {
   if (d->C % 8 != 0 || (double)d->rows * d->C > 2147483647.0 * 8) return CNNK_ERR_UNSUPPORTED;
   return CNNK_OK;
 }
+constexpr int kMaxSumC = 1 << 30;      // columns of sums: slabs of 256 are counted in 32 bits
 int chunks_of(long long rows, int C) {
   const int slabs = (C + 255) / 256;
   long long want = 2048 / slabs, by_rows = (rows + 63) / 64;
@@ -161,7 +162,7 @@ extern "C" int cnnk_dropout_fwd(const cnnk_dropout_desc* d, const void* z, const
 
 extern "C" size_t cnnk_dropout_workspace_bytes(const cnnk_dropout_desc* d) {
   RelDrop dr;
-  if (check(d, &dr) != CNNK_OK) return 0;
+  if (check(d, &dr) != CNNK_OK || d->C > kMaxSumC) return 0;
   return align_up((size_t)chunks_of(d->rows, d->C) * d->C * sizeof(float), 256);
 }
 
@@ -171,6 +172,7 @@ extern "C" int cnnk_dropout_bwd(const cnnk_dropout_desc* d, const void* dy, cons
   const int rc = check(d, &dr);
   if (rc != CNNK_OK) return rc;
   if (!dy || !dz || (dr.q && !rng)) return CNNK_ERR_NULL;
+  if (dbias && d->C > kMaxSumC) return CNNK_ERR_UNSUPPORTED;
   if (dbias && (!ws || ws_bytes < cnnk_dropout_workspace_bytes(d))) return CNNK_ERR_WORKSPACE;
   if (!rel_aligned(dy, 16) || !rel_aligned(dz, 16) || !rel_aligned(rng, 8) || !rel_aligned(dbias, 4) || (dbias && !rel_aligned(ws, 16))) return CNNK_ERR_UNSUPPORTED;
   hipStream_t st = (hipStream_t)stream;

@@ -56,3 +56,13 @@ def test_a_table_that_is_not_learned_needs_the_rows_only():
         with pytest.raises(cnnk.CnnkError) as e:
             call(ws_bytes, dtable)
         assert e.value.status == status
+
+
+def test_sums_of_too_many_columns_are_refused():
+    """A slab of 256 columns past 2^31 - 1: with dbias there are 2^30 at most."""
+    for C, ok in ((1 << 30, True), ((1 << 30) + 8, False), ((1 << 31) - 8, False)):
+        d = rel.dropout_desc(1, C, cnnk.F32, 0.1)
+        assert (rel.cnnk_dropout_workspace_bytes(d) == 4 * C) == ok and (ok or rel.cnnk_dropout_workspace_bytes(d) == 0)
+        with pytest.raises(cnnk.CnnkError) as e:
+            rel.cnnk_dropout_bwd(d, A, A, A, A, None, 0)
+        assert e.value.status == (4 if ok else 3)
